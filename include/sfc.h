@@ -287,6 +287,64 @@ sfc_status sfc_conv2d_stages(const sfc_plan_t* plan, const int8_t* x_dev, float 
 sfc_status sfc_tap_info(const sfc_plan_t* plan, const void* workspace_dev, int32_t which,
                         const void** ptr, int32_t* elem_bytes, int64_t dims[5], int64_t strides[5]);
 
+/* ---- Operators around the frozen convolutions: group norm, low-rank adapters, distillation ----
+ *
+ * What is tuned and served beside a quantized network's convolutions.  The descriptions are plain
+ * structures that are checked in every call; there is no plan.  Strides are in elements; pointers are
+ * aligned to their elements (16-byte alignment is faster, no more); sums, statistics and norms are kept
+ * in 32 bits.  The calls allocate nothing, never synchronize and may be captured into a graph; workspaces
+ * need no clearing.  The same inputs give the same bits in every run. */
+
+typedef enum { SFC_TYPE_F32 = 0, SFC_TYPE_F16 = 1, SFC_TYPE_BF16 = 2, SFC_TYPE_I8 = 3 } sfc_type;
+typedef enum {
+  SFC_LAYOUT_NCHW = 0, /* planes: a convolution's own layout */
+  SFC_LAYOUT_NHWC = 1  /* channels last */
+} sfc_layout;
+typedef enum {
+  SFC_ACTIVATION_NONE = 0,
+  SFC_ACTIVATION_RELU = 1,
+  SFC_ACTIVATION_SILU = 2, /* z / (1 + exp(-z)) */
+  SFC_ACTIVATION_GELU = 3  /* z (1 + erf(z / sqrt 2)) / 2 */
+} sfc_activation;
+
+/* Group norm with an activation.  Over the C / groups channels and all H W pixels of an image's group:
+ *
+ *   h = (x - mean) / sqrt(var + eps),   z = h weight[c] + bias[c],   y = activation(z)
+ *
+ * Types: x in float32, float16 or bfloat16; y in x's type, or the next convolution's int8 activations,
+ * clamp(round-half-even(y / y_scale), -127, 127), or, from float32, either 16-bit type.  int8 and 16-bit
+ * outputs from float32 are forward only.  Layouts may differ forward: planes out of a convolution into
+ * channels last, or channels last into a convolution's int8 planes; int8 is planes always.
+ * Limits: C / groups <= 4096 channels, a group of fewer than 2^30 values, N groups below 2^26, N C H W at most
+ * 2^34.  y_dev may be x_dev where type, layout and strides are one. */
+typedef struct {
+  int32_t N, C, H, W, groups; /* N, H and W may be 0; groups divides C */
+  int32_t x_type, y_type;     /* sfc_type */
+  int32_t x_layout, y_layout; /* sfc_layout */
+  int32_t activation;         /* sfc_activation */
+  float eps;                  /* >= 0 */
+  float y_scale;              /* int8 output: > 0; else not looked at */
+  /* from image to image, and from row to row: of pixels (NHWC) or planes (NCHW).  0: dense.  A row's own
+   * elements lie side by side. */
+  int64_t x_image_stride, x_row_stride, y_image_stride, y_row_stride;
+} sfc_group_norm_desc;
+
+/* Bytes of workspace (device, 16-byte aligned) of the two calls; either pointer may be NULL. */
+sfc_status sfc_group_norm_sizes(const sfc_group_norm_desc* desc, size_t* forward_bytes,
+                                size_t* backward_bytes);
+/* weight_dev, bias_dev: float32 [C], or NULL for ones and zeros.  stats_dev: float32 [N][groups][2], receives
+ * mean and 1 / sqrt(var + eps), which the backward call takes. */
+sfc_status sfc_group_norm(const sfc_group_norm_desc* desc, const void* x_dev, const float* weight_dev,
+                          const float* bias_dev, void* y_dev, float* stats_dev, void* workspace_dev,
+                          size_t workspace_bytes, void* stream);
+/* From y's gradient dy_dev (y's strides) and the forward call's x and statistics: dx_dev (x's type and strides),
+ * and dweight_dev, dbias_dev, float32 [C], sums over all images (either may be NULL).  One layout and one
+ * type (SFC_EUNSUPPORTED otherwise). */
+sfc_status sfc_group_norm_backward(const sfc_group_norm_desc* desc, const void* x_dev, const void* dy_dev,
+                                   const float* weight_dev, const float* bias_dev, const float* stats_dev,
+                                   void* dx_dev, float* dweight_dev, float* dbias_dev, void* workspace_dev,
+                                   size_t workspace_bytes, void* stream);
+
 /* Measurement aid: a plain streaming copy of `bytes` (a multiple of 16, both
  * pointers 16-byte aligned) from src_dev to dst_dev on `stream`.  It reads and
  * writes every byte exactly once, so hardware byte counters and achieved-bandwidth

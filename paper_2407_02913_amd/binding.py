@@ -42,6 +42,7 @@ EXPORTS = (
     "sfc_group_scales",
     "sfc_calibrate_act_scales", "sfc_calibrate_filter_scales", "sfc_transform_filter",
     "sfc_conv2d_nchw", "sfc_conv2d_nchw_static", "sfc_conv2d_stages", "sfc_tap_info", "sfc_stream_copy", "sfc_status_string",
+    "sfc_group_norm_sizes", "sfc_group_norm", "sfc_group_norm_backward",
 )
 
 
@@ -49,6 +50,18 @@ class ConvDesc(C.Structure):
     _fields_ = [(n, C.c_int32) for n in
                 ("N", "Cin", "Cout", "H", "W", "alg", "mode", "out", "path", "per_channel_wscale",
                  "transform_bits", "flags")]
+
+
+TYPE_F32, TYPE_F16, TYPE_BF16, TYPE_I8 = 0, 1, 2, 3
+LAYOUT_NCHW, LAYOUT_NHWC = 0, 1
+ACTIVATION = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("N", "C", "H", "W", "groups", "x_type", "y_type", "x_layout", "y_layout",
+                                          "activation")]
+                + [(n, C.c_float) for n in ("eps", "y_scale")]
+                + [(n, C.c_int64) for n in ("x_image_stride", "x_row_stride", "y_image_stride", "y_row_stride")])
 
 
 class SfcError(RuntimeError):
@@ -104,6 +117,13 @@ def load(force: bool = False):
     lib.sfc_tap_info.restype = i32
     lib.sfc_stream_copy.argtypes = [vp, vp, C.c_size_t, vp]
     lib.sfc_stream_copy.restype = i32
+    size_p = C.POINTER(C.c_size_t)
+    lib.sfc_group_norm_sizes.argtypes = [vp, size_p, size_p]
+    lib.sfc_group_norm_sizes.restype = i32
+    lib.sfc_group_norm.argtypes = [vp] * 7 + [C.c_size_t, vp]
+    lib.sfc_group_norm.restype = i32
+    lib.sfc_group_norm_backward.argtypes = [vp] * 10 + [C.c_size_t, vp]
+    lib.sfc_group_norm_backward.restype = i32
     lib.sfc_status_string.argtypes = [i32]
     lib.sfc_status_string.restype = C.c_char_p
     _lib = lib

@@ -1,0 +1,259 @@
+// Group norm with an activation: what the kernels and their launchers share.
+#pragma once
+#include "sfc_values.hpp"
+
+namespace sfc {
+
+// Division by a number that is the same for a whole launch, exact for 0 <= n < 2^31: the multiplier is
+// floor(2^(31+s) / d) + 1 with s = ceil(log2 d), its excess below 2^s.
+struct FastDiv {
+  unsigned d, m, s;
+  static FastDiv by(unsigned d) {
+    unsigned s = 0;
+    while ((1u << s) < d) ++s;
+    return {d, d > 1 ? (unsigned)((1ull << (31 + s)) / d + 1) : 0u, s};
+  }
+  __device__ __forceinline__ int operator()(int n) const {
+    return d == 1 ? n : (int)(__umulhi((unsigned)n, m) >> (s - 1));
+  }
+};
+
+struct NormArgs {
+  const void* x;
+  const void* dy;       // backward
+  void* y;              // forward: y; backward: dx
+  const float* weight;  // [C] or null: ones
+  const float* bias;    // [C] or null: zeros
+  float* stats;         // [N][G][2]: mean, 1 / sqrt(var + eps)
+  float* part;          // workspace: what the first of two kernels leaves for the second, by [N][G][chunks]:
+                        // forward float4 (mean, sum of squares about it, count), backward float2
+  float* part_c;        // backward: sums of a channel, float2, indexed by c_image, c_chunk, c_group
+  float* dweight;       // [C] or null
+  float* dbias;         // [C] or null
+  int N, C, P, G, cpg;  // P: pixels of a map; cpg: channels of a group
+  int64_t xs_n, xs_r, ys_n, ys_r;  // strides of x and dx; of y and dy
+  int64_t x_end, y_end;            // elements from the tensor's first to behind its last
+  int64_t c_image, c_chunk, c_group;
+  int activation;
+  float eps, inv_y;
+  int chunks, per;         // parts of a group, and a part's length (channels last: pixels; planes: vectors)
+  int slab, slabs, lanes;  // channels last: groups and number of slabs; log2 of lanes for a row of a slab
+  int segments, vps;       // planes: runs of a group, and vectors in one
+  FastDiv by_vps, by_p;    // vector -> run; planes: element of a group -> channel; channels last: channel -> group
+  int threads, per_thread; // resident kernels: of a workgroup, and vectors of a thread (0: two kernels)
+  int finals;              // workgroups in front that add up part_c
+};
+
+// y = act(z)
+__device__ __forceinline__ float fast_sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+}
+
+// (1 + erf(z / sqrt 2)) / 2 and exp(-z^2 / 2), by the rational form 7.1.26 of Abramowitz and Stegun's
+// Handbook of Mathematical Functions (absolute error of erf below 1.5e-7); the tail of negative z is the
+// product itself, not a difference.
+__device__ __forceinline__ float normal_cdf(float z, float* bell) {
+  const float x = fabsf(z) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
+  const float e = __expf(-x * x);
+  *bell = e;
+  float q = fmaf(1.061405429f, t, -1.453152027f);
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  const float tail = 0.5f * q * t * e;
+  return z < 0.0f ? tail : 1.0f - tail;
+}
+
+// Activation of V values; the branch is the same for a whole launch.
+template <int V>
+__device__ __forceinline__ void activate(int activation, float (&z)[V]) {
+  switch (activation) {
+    case 1:
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = z[j] < 0.0f ? 0.0f : z[j];  // (a NaN stays one)
+      break;
+    case 2:
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] *= fast_sigmoid(z[j]);
+      break;
+    case 3:
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float bell;
+        z[j] *= normal_cdf(z[j], &bell);
+      }
+      break;
+    default:
+      break;
+  }
+}
+
+// dz = dy act'(z) of V values, in place of dy.
+template <int V>
+__device__ __forceinline__ void activate_back(int activation, const float (&z)[V], float (&d)[V]) {
+  switch (activation) {
+    case 1:
+#pragma unroll
+      for (int j = 0; j < V; ++j) d[j] = z[j] > 0.0f ? d[j] : 0.0f;
+      break;
+    case 2:
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float s = fast_sigmoid(z[j]);
+        d[j] *= fmaf(z[j] * s, 1.0f - s, s);
+      }
+      break;
+    case 3:
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float bell;
+        const float s = normal_cdf(z[j], &bell);
+        d[j] *= fmaf(z[j] * bell, 0.39894228f, s);
+      }
+      break;
+    default:
+      break;
+  }
+}
+
+// Loaded vectors behind whose last valid element may lie others of the same tensor: read whole unless the
+// tensor ends, cut to the valid ones.
+template <typename T>
+__device__ __forceinline__ raw4 load_cut(const T* p, int valid, int64_t room) {
+  if (valid >= kVec<T>) return load16(p);
+  if (room < kVec<T>) return load_part(p, valid);
+  raw4 r = load16(p);
+  constexpr int per = 4 / (int)sizeof(T);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (per == 1) {
+      if (d >= valid) r[d] = 0u;
+    } else {
+      if (2 * d >= valid) r[d] = 0u;
+      else if (2 * d + 1 >= valid) r[d] &= 0xffffu;
+    }
+  }
+  return r;
+}
+
+// int8 activations of the next convolution: round-half-even(v * inv) within +-127 (quantize_byte's way).
+template <int V>
+__device__ __forceinline__ void store_i8(int8_t* p, const float (&v)[V], float inv, int valid) {
+  constexpr float kMagic = 12582912.0f;
+  unsigned b[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    b[j] = __float_as_uint(
+        __builtin_amdgcn_fmed3f(__fmaf_rn(v[j], inv, kMagic), kMagic - 127.0f, kMagic + 127.0f));
+  if (valid >= V) {
+    typedef unsigned dwords __attribute__((ext_vector_type(V / 4), aligned(1)));
+    dwords o;
+#pragma unroll
+    for (int d = 0; d < V / 4; ++d)
+      o[d] = (b[4 * d] & 255u) | (b[4 * d + 1] & 255u) << 8 | (b[4 * d + 2] & 255u) << 16 | b[4 * d + 3] << 24;
+    *reinterpret_cast<dwords*>(p) = o;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (j < valid) p[j] = (int8_t)b[j];
+}
+
+template <typename TO, int V>
+__device__ __forceinline__ void store_out(TO* p, const float (&v)[V], float inv, int valid) {
+  if constexpr (__is_same(TO, int8_t))
+    store_i8<V>(p, v, inv, valid);
+  else
+    store_vec<TO, V>(p, v, valid);
+}
+
+// Sum of one value a thread over a workgroup, in every thread; `scratch` holds a float per wave and is free
+// again after the next barrier.
+__device__ __forceinline__ float block_sum(float v, float* scratch) {
+  v = wave_sum(v);
+  const int waves = (int)(blockDim.x >> 6);
+  if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float s = 0.0f;
+  for (int i = 0; i < waves; ++i) s += scratch[i];
+  return s;
+}
+
+// Mean and 1 / sqrt(var + eps) of a group from its parts, by `width` neighbouring lanes (a power of two):
+// the mean of means, then squares about it, so nothing large is subtracted.
+__device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g, int lane, int width) {
+  const float4* part = reinterpret_cast<const float4*>(a.part) + ((int64_t)n * a.G + g) * a.chunks;
+  float sum = 0.0f, squares = 0.0f;
+  for (int i = lane; i < a.chunks; i += width) {
+    const float4 p = part[i];
+    sum = fmaf(p.x, p.z, sum);
+  }
+  for (int m = width >> 1; m; m >>= 1) sum += __shfl_xor(sum, m, 64);
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P), mean = sum * inv;
+  for (int i = lane; i < a.chunks; i += width) {
+    const float4 p = part[i];
+    const float d = p.x - mean;
+    squares += fmaf(d * d, p.z, p.y);
+  }
+  for (int m = width >> 1; m; m >>= 1) squares += __shfl_xor(squares, m, 64);
+  return make_float2(mean, 1.0f / sqrtf(fmaf(squares, inv, a.eps)));
+}
+
+// Adds part_c over images and parts: workgroup `block` of the `finals` in front, eight channels.
+__device__ __forceinline__ void channel_sums(const NormArgs& a, int block, float2* scratch) {
+  const int t = threadIdx.x, c = block * 8 + (t & 7), rows = a.N * a.chunks;
+  float s1 = 0.0f, s2 = 0.0f;
+  if (c < a.C) {
+    const float2* at = reinterpret_cast<const float2*>(a.part_c) + (int64_t)(c / a.cpg) * a.c_group + c % a.cpg;
+    const int step = (int)blockDim.x >> 3;
+    int r = t >> 3;
+    for (; r + 3 * step < rows; r += 4 * step) {  // four loads on their way at once
+      float2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int q = r + k * step, n = q / a.chunks;
+        v[k] = at[n * a.c_image + (q - n * a.chunks) * a.c_chunk];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s1 += v[k].x, s2 += v[k].y;
+    }
+    for (; r < rows; r += step) {
+      const int n = r / a.chunks;
+      const float2 v = at[n * a.c_image + (r - n * a.chunks) * a.c_chunk];
+      s1 += v.x, s2 += v.y;
+    }
+  }
+  s1 = wave_sum(s1, 8), s2 = wave_sum(s2, 8);
+  if ((t & 63) < 8) scratch[(t >> 6) * 8 + (t & 7)] = make_float2(s1, s2);
+  __syncthreads();
+  if (t < 8 && c < a.C) {
+    float2 s = make_float2(0.0f, 0.0f);
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s.x += scratch[w * 8 + t].x, s.y += scratch[w * 8 + t].y;
+    if (a.dbias) a.dbias[c] = s.x;
+    if (a.dweight) a.dweight[c] = s.y;
+  }
+}
+
+// Types of a call: what a kernel is instantiated for.
+enum NormType { kNormF32 = 0, kNormF16 = 1, kNormBF16 = 2, kNormI8 = 3 };
+
+// The kernels of a layout (sfc_norm_planes.hip, sfc_norm_last.hip, sfc_norm_cross.hip); the plan fields of
+// the arguments are theirs to fill in, and plan_* give the workspace's bytes.
+size_t plan_norm_planes(NormArgs* a, int x_size, bool resident_allowed);
+size_t plan_norm_last(NormArgs* a, int x_size, bool resident_allowed);
+size_t plan_norm_planes_backward(NormArgs* a, int x_size);
+size_t plan_norm_last_backward(NormArgs* a, int x_size);
+hipError_t launch_norm_planes(const NormArgs& a, int x_type, int y_type, hipStream_t s);
+hipError_t launch_norm_last(const NormArgs& a, int x_type, int y_type, hipStream_t s);
+// statistics alone, left in part for the kernel that changes the layout
+hipError_t launch_norm_planes_stats(const NormArgs& a, int x_type, hipStream_t s);
+hipError_t launch_norm_last_stats(const NormArgs& a, int x_type, hipStream_t s);
+hipError_t launch_norm_cross(const NormArgs& a, int x_type, int y_type, bool from_last, hipStream_t s);
+hipError_t launch_norm_planes_backward(const NormArgs& a, int x_type, hipStream_t s);
+hipError_t launch_norm_last_backward(const NormArgs& a, int x_type, hipStream_t s);
+
+// zeros into count floats
+hipError_t launch_zeros(float* to, int count, hipStream_t s);
+
+}  // namespace sfc

@@ -1,0 +1,173 @@
+// C entry points of group norm: checks, workspace sizes, choice of kernels.
+#include "sfc.h"
+#include "sfc_norm.hpp"
+
+namespace {
+
+using sfc::NormArgs;
+
+int type_size(int type) {
+  return type == SFC_TYPE_F32 ? 4 : type == SFC_TYPE_F16 || type == SFC_TYPE_BF16 ? 2 : type == SFC_TYPE_I8 ? 1 : 0;
+}
+
+bool aligned(const void* p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
+
+// Strides of a tensor (0: dense) and the elements from its first to behind its last; false: rows overlap.
+bool strides_of(const sfc_group_norm_desc& d, int layout, int64_t image, int64_t row, int64_t* image_out,
+                int64_t* row_out, int64_t* end) {
+  const int64_t pixels = (int64_t)d.H * d.W;
+  const int64_t length = layout == SFC_LAYOUT_NHWC ? d.C : pixels, rows = layout == SFC_LAYOUT_NHWC ? pixels : d.C;
+  if (image < 0 || row < 0) return false;
+  *row_out = row ? row : length;
+  *image_out = image ? image : *row_out * rows;
+  if (*row_out < length || *image_out < length) return false;
+  // (no tensor is larger: 2^36 bytes keep every count below within its type)
+  if (rows > 0 && *row_out > ((int64_t)1 << 36) / rows) return false;
+  if (d.N > 0 && *image_out > ((int64_t)1 << 36) / d.N) return false;
+  *end = (int64_t)(d.N - 1) * *image_out + (rows - 1) * *row_out + length;
+  return true;
+}
+
+// Fills in what follows from the description alone.  *nothing: no image or no pixel.
+sfc_status describe(const sfc_group_norm_desc* d, NormArgs* a, bool* nothing) {
+  if (!d) return SFC_EINVAL;
+  if (d->N < 0 || d->C <= 0 || d->H < 0 || d->W < 0 || d->groups <= 0 || d->C % d->groups != 0) return SFC_EINVAL;
+  if (type_size(d->x_type) < 2 || type_size(d->y_type) == 0) return SFC_EINVAL;
+  if (d->x_layout != SFC_LAYOUT_NCHW && d->x_layout != SFC_LAYOUT_NHWC) return SFC_EINVAL;
+  if (d->y_layout != SFC_LAYOUT_NCHW && d->y_layout != SFC_LAYOUT_NHWC) return SFC_EINVAL;
+  if (d->activation < SFC_ACTIVATION_NONE || d->activation > SFC_ACTIVATION_GELU) return SFC_EINVAL;
+  if (!(d->eps >= 0.0f)) return SFC_EINVAL;
+  const bool i8 = d->y_type == SFC_TYPE_I8;
+  if (i8 && !(d->y_scale > 0.0f)) return SFC_EINVAL;
+  if (i8 && d->y_layout != SFC_LAYOUT_NCHW) return SFC_EUNSUPPORTED;
+  if (!i8 && d->y_type != d->x_type && d->x_type != SFC_TYPE_F32) return SFC_EUNSUPPORTED;
+  const int64_t pixels = (int64_t)d->H * d->W, cpg = d->C / d->groups;
+  if (cpg > 4096 || pixels * cpg >= ((int64_t)1 << 30)) return SFC_EUNSUPPORTED;
+  if ((int64_t)d->N * d->groups >= ((int64_t)1 << 26)) return SFC_EUNSUPPORTED;
+  if ((int64_t)d->N * d->C > ((int64_t)1 << 34) / (pixels > 0 ? pixels : 1)) return SFC_EUNSUPPORTED;
+  *a = NormArgs{};
+  if (!strides_of(*d, d->x_layout, d->x_image_stride, d->x_row_stride, &a->xs_n, &a->xs_r, &a->x_end) ||
+      !strides_of(*d, d->y_layout, d->y_image_stride, d->y_row_stride, &a->ys_n, &a->ys_r, &a->y_end))
+    return SFC_EINVAL;
+  a->N = d->N;
+  a->C = d->C;
+  a->P = (int)pixels;
+  a->G = d->groups;
+  a->cpg = (int)cpg;
+  a->activation = d->activation;
+  a->eps = d->eps;
+  a->inv_y = i8 ? 1.0f / d->y_scale : 0.0f;
+  *nothing = d->N == 0 || pixels == 0;
+  return SFC_OK;
+}
+
+bool crosses(const sfc_group_norm_desc& d) { return d.x_layout != d.y_layout; }
+
+bool one_kind(const sfc_group_norm_desc& d) { return !crosses(d) && d.x_type == d.y_type; }
+
+size_t plan_forward(const sfc_group_norm_desc& d, NormArgs* a) {
+  const int size = type_size(d.x_type);
+  return d.x_layout == SFC_LAYOUT_NHWC ? sfc::plan_norm_last(a, size, !crosses(d))
+                                       : sfc::plan_norm_planes(a, size, !crosses(d));
+}
+
+size_t plan_backward(const sfc_group_norm_desc& d, NormArgs* a) {
+  const int size = type_size(d.x_type);
+  return d.x_layout == SFC_LAYOUT_NHWC ? sfc::plan_norm_last_backward(a, size)
+                                       : sfc::plan_norm_planes_backward(a, size);
+}
+
+}  // namespace
+
+extern "C" {
+
+sfc_status sfc_group_norm_sizes(const sfc_group_norm_desc* desc, size_t* forward_bytes, size_t* backward_bytes) {
+  NormArgs a;
+  bool nothing;
+  const sfc_status st = describe(desc, &a, &nothing);
+  if (st != SFC_OK) return st;
+  if (forward_bytes) {
+    NormArgs f = a;
+    *forward_bytes = nothing ? 0 : plan_forward(*desc, &f);
+  }
+  if (backward_bytes) {
+    NormArgs b = a;
+    *backward_bytes = nothing || !one_kind(*desc) ? 0 : plan_backward(*desc, &b);
+  }
+  return SFC_OK;
+}
+
+sfc_status sfc_group_norm(const sfc_group_norm_desc* desc, const void* x_dev, const float* weight_dev,
+                          const float* bias_dev, void* y_dev, float* stats_dev, void* workspace_dev,
+                          size_t workspace_bytes, void* stream) {
+  NormArgs a;
+  bool nothing;
+  const sfc_status st = describe(desc, &a, &nothing);
+  if (st != SFC_OK) return st;
+  if (nothing) return SFC_OK;
+  if (!x_dev || !y_dev || !stats_dev) return SFC_EINVAL;
+  if (!aligned(x_dev, type_size(desc->x_type)) || !aligned(y_dev, type_size(desc->y_type)) ||
+      !aligned(weight_dev, 4) || !aligned(bias_dev, 4) || !aligned(stats_dev, 8) || !aligned(workspace_dev, 16))
+    return SFC_EINVAL;
+  const size_t need = plan_forward(*desc, &a);
+  if (need > 0 && (!workspace_dev || workspace_bytes < need)) return SFC_EWORKSPACE;
+  a.x = x_dev;
+  a.y = y_dev;
+  a.weight = weight_dev;
+  a.bias = bias_dev;
+  a.stats = stats_dev;
+  a.part = static_cast<float*>(workspace_dev);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const bool last = desc->x_layout == SFC_LAYOUT_NHWC;
+  hipError_t e;
+  if (crosses(*desc)) {
+    e = last ? sfc::launch_norm_last_stats(a, desc->x_type, s) : sfc::launch_norm_planes_stats(a, desc->x_type, s);
+    if (e == hipSuccess) e = sfc::launch_norm_cross(a, desc->x_type, desc->y_type, last, s);
+  } else {
+    e = last ? sfc::launch_norm_last(a, desc->x_type, desc->y_type, s)
+             : sfc::launch_norm_planes(a, desc->x_type, desc->y_type, s);
+  }
+  return e == hipSuccess ? SFC_OK : SFC_EHIP;
+}
+
+sfc_status sfc_group_norm_backward(const sfc_group_norm_desc* desc, const void* x_dev, const void* dy_dev,
+                                   const float* weight_dev, const float* bias_dev, const float* stats_dev,
+                                   void* dx_dev, float* dweight_dev, float* dbias_dev, void* workspace_dev,
+                                   size_t workspace_bytes, void* stream) {
+  NormArgs a;
+  bool nothing;
+  const sfc_status st = describe(desc, &a, &nothing);
+  if (st != SFC_OK) return st;
+  if (!one_kind(*desc)) return SFC_EUNSUPPORTED;
+  if (!aligned(weight_dev, 4) || !aligned(bias_dev, 4) || !aligned(dweight_dev, 4) || !aligned(dbias_dev, 4))
+    return SFC_EINVAL;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (nothing) {  // sums over nothing
+    if (dweight_dev && sfc::launch_zeros(dweight_dev, a.C, s) != hipSuccess) return SFC_EHIP;
+    if (dbias_dev && sfc::launch_zeros(dbias_dev, a.C, s) != hipSuccess) return SFC_EHIP;
+    return SFC_OK;
+  }
+  if (!x_dev || !dy_dev || !dx_dev || !stats_dev) return SFC_EINVAL;
+  const int size = type_size(desc->x_type);
+  if (!aligned(x_dev, size) || !aligned(dy_dev, size) || !aligned(dx_dev, size) || !aligned(stats_dev, 8) ||
+      !aligned(workspace_dev, 16))
+    return SFC_EINVAL;
+  const size_t need = plan_backward(*desc, &a);
+  if (!workspace_dev || workspace_bytes < need) return SFC_EWORKSPACE;
+  a.x = x_dev;
+  a.dy = dy_dev;
+  a.y = dx_dev;
+  a.weight = weight_dev;
+  a.bias = bias_dev;
+  a.stats = const_cast<float*>(stats_dev);
+  a.dweight = dweight_dev;
+  a.dbias = dbias_dev;
+  // the channels' sums, then the groups' (which the kernels that read a group once do without)
+  a.part_c = static_cast<float*>(workspace_dev);
+  a.part = a.part_c + 2 * (int64_t)a.N * a.C * a.chunks;
+  const hipError_t e = desc->x_layout == SFC_LAYOUT_NHWC ? sfc::launch_norm_last_backward(a, desc->x_type, s)
+                                                         : sfc::launch_norm_planes_backward(a, desc->x_type, s);
+  return e == hipSuccess ? SFC_OK : SFC_EHIP;
+}
+
+}  // extern "C"

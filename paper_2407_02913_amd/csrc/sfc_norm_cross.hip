@@ -1,0 +1,173 @@
+// Group norm's second kernel where the output's layout is not the input's: channels last into the next convolution's
+// planes, or planes into channels last.
+//
+// A tile is 64 places of the input's inner axis by 64 (int8: 128) of its outer one, and passes through LDS: a lane
+// loads 16 bytes along the inner axis at as many outer places as outputs fill a dword, packs them along the outer
+// axis, and rows of the tile leave as 128 or 256 contiguous bytes along the output's inner axis.  One dword of padding
+// a row keeps the packed writes (a row each) and the reads (along a row) on different banks.
+#include "sfc_norm.hpp"
+
+namespace sfc {
+namespace {
+
+constexpr int kInner = 64;
+
+template <typename TO>
+constexpr int kPack = 4 / (int)sizeof(TO);
+template <typename TO>
+constexpr int kOuter = sizeof(TO) == 1 ? 128 : 64;
+
+// Outputs that fill a dword.
+template <typename TO>
+__device__ __forceinline__ unsigned pack_outputs(const float (&v)[kPack<TO>], float inv) {
+  if constexpr (__is_same(TO, int8_t)) {
+    constexpr float kMagic = 12582912.0f;
+    unsigned o = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      o |= (__float_as_uint(__builtin_amdgcn_fmed3f(__fmaf_rn(v[i], inv, kMagic), kMagic - 127.0f,
+                                                    kMagic + 127.0f)) & 255u) << (8 * i);
+    return o;
+  } else if constexpr (sizeof(TO) == 2) {
+    return (unsigned)__builtin_bit_cast(unsigned short, (TO)v[0]) |
+           (unsigned)__builtin_bit_cast(unsigned short, (TO)v[1]) << 16;
+  } else {
+    return __float_as_uint(v[0]);
+  }
+}
+
+template <typename TI, typename TO, bool FROM_LAST>
+__global__ __launch_bounds__(256) void cross_apply(NormArgs a, int parts, int tiles_c, int tiles_p) {
+  constexpr int V = kVec<TI>, K = kPack<TO>, OUTER = kOuter<TO>, PITCH = OUTER / K + 1;
+  constexpr int CH = FROM_LAST ? kInner : OUTER, PX = FROM_LAST ? OUTER : kInner;  // channels and pixels of a tile
+  __shared__ unsigned tile[kInner * PITCH];
+  __shared__ float4 of_channel[CH];  // mean, 1 / sd, weight, bias
+  __shared__ float2 of_group[CH];
+  const int t = threadIdx.x;
+  int id = blockIdx.x;
+  const int part = id % parts;
+  id /= parts;
+  const int n = id / tiles_c, c0 = (id - n * tiles_c) * CH, channels = min(CH, a.C - c0);
+  const int g0 = c0 / a.cpg, groups = (c0 + channels - 1) / a.cpg - g0 + 1;
+  int width = 64;
+  while (width > 1 && groups * width > 256) width >>= 1;
+  for (int g = t / width; g < groups; g += 256 / width) {
+    const float2 s = combine_parts(a, n, g0 + g, t & (width - 1), width);
+    if ((t & (width - 1)) == 0) {
+      of_group[g] = s;
+      // (the tile that holds a group's first channel keeps its statistics)
+      if (part == 0 && (g0 + g) * a.cpg >= c0) reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + g0 + g] = s;
+    }
+  }
+  __syncthreads();
+  for (int c = t; c < CH; c += 256) {
+    const int at = c0 + min(c, channels - 1);
+    const float2 s = of_group[at / a.cpg - g0];
+    of_channel[c] = make_float4(s.x, s.y, a.weight ? a.weight[at] : 1.0f, a.bias ? a.bias[at] : 0.0f);
+  }
+  __syncthreads();
+  const TI* x = static_cast<const TI*>(a.x) + n * a.xs_n;
+  TO* y = static_cast<TO*>(a.y) + n * a.ys_n;
+  const int64_t room = a.x_end - n * a.xs_n;
+  for (int tp = part; tp < tiles_p; tp += parts) {
+    const int p0 = tp * PX, pixels = min(PX, a.P - p0);
+    const int i0 = FROM_LAST ? c0 : p0, inner = FROM_LAST ? channels : pixels;
+    const int o0 = FROM_LAST ? p0 : c0, outer = FROM_LAST ? pixels : channels;
+    constexpr int TASKS = (kInner / V) * (OUTER / K);
+#pragma unroll
+    for (int u = 0; u < TASKS / 256; ++u) {
+      const int task = t + u * 256, i = task % (kInner / V) * V, o = task / (kInner / V) * K;
+      if (i < inner && o < outer) {
+        float v[K][V];
+#pragma unroll
+        for (int e = 0; e < K; ++e) {
+          const int64_t at = (int64_t)(o0 + min(o + e, outer - 1)) * a.xs_r + i0 + i;
+          const raw4 r = load_cut(x + at, min(V, inner - i), room - at);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float4 s = of_channel[FROM_LAST ? i + j : min(o + e, outer - 1)];
+            v[e][j] = fmaf((element<TI>(r, j) - s.x) * s.y, s.z, s.w);
+          }
+          activate<V>(a.activation, v[e]);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          float w[K];
+#pragma unroll
+          for (int e = 0; e < K; ++e) w[e] = v[e][j];
+          tile[(i + j) * PITCH + o / K] = pack_outputs<TO>(w, a.inv_y);
+        }
+      }
+    }
+    __syncthreads();
+    constexpr int E = 16 / (int)sizeof(TO);  // outputs of a store
+    for (int s = t; s < kInner * (OUTER / E); s += 256) {
+      const int row = s / (OUTER / E), o = s % (OUTER / E) * E;
+      if (row < inner && o < outer) {
+        raw4 r;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) r[d] = tile[row * PITCH + o / K + d];
+        TO* to = y + (int64_t)(i0 + row) * a.ys_r + o0 + o;
+        const int valid = outer - o;
+        if (valid >= E) {
+          *reinterpret_cast<raw16<TO>*>(to) = r;
+        } else {
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            if (j < valid) {
+              if constexpr (sizeof(TO) == 4) reinterpret_cast<unsigned*>(to)[j] = r[j];
+              else if constexpr (sizeof(TO) == 2)
+                reinterpret_cast<unsigned short*>(to)[j] = (unsigned short)(r[j / 2] >> (16 * (j % 2)));
+              else
+                to[j] = (TO)(r[j / 4] >> (8 * (j % 4)));
+            }
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <typename TI, typename TO, bool FROM_LAST>
+hipError_t run_cross(const NormArgs& a, hipStream_t s) {
+  constexpr int CH = FROM_LAST ? kInner : kOuter<TO>, PX = FROM_LAST ? kOuter<TO> : kInner;
+  const int tiles_c = (a.C + CH - 1) / CH, tiles_p = (a.P + PX - 1) / PX;
+  // some 2048 workgroups; each joins the parts of its groups' statistics once
+  const int64_t columns = (int64_t)a.N * tiles_c;
+  int64_t parts = (2048 + columns - 1) / columns;
+  if (parts > tiles_p) parts = tiles_p;
+  cross_apply<TI, TO, FROM_LAST><<<dim3((unsigned)(columns * parts)), 256, 0, s>>>(a, (int)parts, tiles_c, tiles_p);
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void zeros(float* to, int count) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < count) to[i] = 0.0f;
+}
+
+}  // namespace
+
+hipError_t launch_zeros(float* to, int count, hipStream_t s) {
+  zeros<<<dim3((unsigned)(count + 255) / 256u), 256, 0, s>>>(to, count);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_cross(const NormArgs& a, int x_type, int y_type, bool from_last, hipStream_t s) {
+  if (from_last) {
+    if (y_type == kNormI8) {
+      if (x_type == kNormF32) return run_cross<float, int8_t, true>(a, s);
+      return x_type == kNormF16 ? run_cross<f16, int8_t, true>(a, s) : run_cross<bf16, int8_t, true>(a, s);
+    }
+    if (x_type == kNormF16) return run_cross<f16, f16, true>(a, s);
+    if (x_type == kNormBF16) return run_cross<bf16, bf16, true>(a, s);
+    if (y_type == kNormF16) return run_cross<float, f16, true>(a, s);
+    return y_type == kNormBF16 ? run_cross<float, bf16, true>(a, s) : run_cross<float, float, true>(a, s);
+  }
+  if (x_type == kNormF16) return run_cross<f16, f16, false>(a, s);
+  if (x_type == kNormBF16) return run_cross<bf16, bf16, false>(a, s);
+  if (y_type == kNormF16) return run_cross<float, f16, false>(a, s);
+  return y_type == kNormBF16 ? run_cross<float, bf16, false>(a, s) : run_cross<float, float, false>(a, s);
+}
+
+}  // namespace sfc

@@ -1,0 +1,578 @@
+// Group norm with an activation, channels last (NHWC).
+//
+// A workgroup owns a slab: neighbouring whole groups, so that a pixel's row of the slab is one contiguous piece, and
+// all or a part of the pixels.  The row is cut into vectors of 16 bytes; a thread keeps one vector column, hence the
+// same channels for every pixel it sees, and their weights in registers.  Lanes for a row are rounded up to a power of
+// two, so that threads of one column are found by lane number: sums run over pixels within the thread, over the wave's
+// rows by lane exchange, over waves through LDS, and last over a group's channels, whatever their count (a vector may
+// hold several groups, a group several vectors).
+//
+// A slab that fits the registers of a workgroup is read once (last_resident); else two kernels.
+#include "sfc_norm.hpp"
+
+namespace sfc {
+namespace {
+
+// A thread's place in its workgroup's slab.
+template <typename T>
+struct Column {
+  int n, g0, groups, width;  // image, first group, groups of the slab, channels of the slab
+  int col, row, rows;        // vector column, first pixel, pixels of the workgroup at a time
+  int c, valid;              // channel of the vector's first element, its elements within the slab
+  __device__ __forceinline__ Column(const NormArgs& a, int n_, int slab) {
+    n = n_;
+    g0 = slab * a.slab;
+    groups = min(a.slab, a.G - g0);
+    width = groups * a.cpg;
+    const int t = threadIdx.x;
+    col = t & ((1 << a.lanes) - 1);
+    row = t >> a.lanes;
+    rows = (int)blockDim.x >> a.lanes;
+    c = g0 * a.cpg + col * kVec<T>;
+    valid = max(0, min(kVec<T>, width - col * kVec<T>));
+  }
+};
+
+// Adds v over the workgroup's pixels: lanes of a wave, then what the waves leave in LDS by channel of the slab.
+// Returns the number of rows there (each `pitch` floats) to be added by the reader.  Ends with a barrier.
+template <int V>
+__device__ __forceinline__ int slab_rows(const NormArgs& a, float (&v)[V], float* rows) {
+  const int lanes = 1 << a.lanes, pitch = lanes * V, t = threadIdx.x, col = t & (lanes - 1);
+  if (lanes < 64) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = wave_sum(v[j], lanes);
+  }
+  const int slot = lanes < 64 ? t >> 6 : t >> a.lanes;
+  if (lanes >= 64 || (t & 63) < lanes) {
+    float* at = rows + slot * pitch + col * V;
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(at + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  }
+  __syncthreads();
+  return lanes < 64 ? (int)blockDim.x >> 6 : (int)blockDim.x >> a.lanes;
+}
+
+// Lanes that add a group.
+__device__ __forceinline__ int lanes_of(int groups) {
+  int width = 64;
+  while (width > 1 && groups * width > (int)blockDim.x) width >>= 1;
+  return width;
+}
+
+// Sums over the slab's groups of a value that every thread holds for its channels; in `out` after the call.
+template <int V>
+__device__ __forceinline__ void slab_sums(const NormArgs& a, int groups, float (&v)[V], float* rows, float* out) {
+  const int count = slab_rows<V>(a, v, rows), pitch = V << a.lanes;
+  const int width = lanes_of(groups), lane = threadIdx.x & (width - 1);
+  for (int g = threadIdx.x / width; g < groups; g += (int)blockDim.x / width) {
+    float s = 0.0f;
+    for (int r = 0; r < count; ++r)
+      for (int j = lane; j < a.cpg; j += width) s += rows[r * pitch + g * a.cpg + j];
+    for (int m = width >> 1; m; m >>= 1) s += __shfl_xor(s, m, 64);
+    if (lane == 0) out[g] = s;
+  }
+  __syncthreads();
+}
+
+template <typename T>
+__device__ __forceinline__ void affine_of(const NormArgs& a, const Column<T>& k, float (&w)[kVec<T>],
+                                          float (&b)[kVec<T>]) {
+#pragma unroll
+  for (int j = 0; j < kVec<T>; ++j) {
+    const int c = min(k.c + j, a.C - 1);
+    w[j] = a.weight ? a.weight[c] : 1.0f;
+    b[j] = a.bias ? a.bias[c] : 0.0f;
+  }
+}
+
+// The slab's group of each of a thread's channels (a channel past the slab: its last group).
+template <typename T>
+__device__ __forceinline__ void groups_of(const NormArgs& a, const Column<T>& k, int (&group)[kVec<T>]) {
+#pragma unroll
+  for (int j = 0; j < kVec<T>; ++j) group[j] = min(a.by_p((k.col * kVec<T> + j)), k.groups - 1);
+}
+
+template <typename TI, typename TO, int NV>
+__global__ __launch_bounds__(1024) void last_resident(NormArgs a) {
+  constexpr int V = kVec<TI>;
+  extern __shared__ float4 lds[];
+  const int n = blockIdx.x / a.slabs;
+  const Column<TI> k(a, n, blockIdx.x - n * a.slabs);
+  const TI* x = static_cast<const TI*>(a.x) + n * a.xs_n + k.c;
+  TO* y = static_cast<TO*>(a.y) + n * a.ys_n + k.c;
+  const int64_t room = a.x_end - n * a.xs_n - k.c;
+  raw4 raw[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int p = k.row + u * k.rows;
+    raw[u] = raw4{0u, 0u, 0u, 0u};
+    if (p < a.P && k.valid) raw[u] = load_cut(x + p * a.xs_r, k.valid, room - p * a.xs_r);
+  }
+  float w[V], b[V];
+  int group[V];
+  affine_of<TI>(a, k, w, b);
+  groups_of<TI>(a, k, group);
+  float* means = reinterpret_cast<float*>(lds);
+  float* rstds = means + a.slab;
+  float* rows = means + (2 * a.slab + 3) / 4 * 4;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = 0.0f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] += element<TI>(raw[u], j);
+  slab_sums<V>(a, k.groups, v, rows, means);
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  float mean[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) mean[j] = means[group[j]] * inv, v[j] = 0.0f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    if (k.row + u * k.rows < a.P) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = element<TI>(raw[u], j) - mean[j];
+        v[j] = fmaf(d, d, v[j]);
+      }
+    }
+  }
+  slab_sums<V>(a, k.groups, v, rows, rstds);
+  float rstd[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(fmaf(rstds[group[j]], inv, a.eps));
+  for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
+    reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] =
+        make_float2(means[g] * inv, 1.0f / sqrtf(fmaf(rstds[g], inv, a.eps)));
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int p = k.row + u * k.rows;
+    if (p < a.P && k.valid) {
+      float z[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) z[j] = fmaf((element<TI>(raw[u], j) - mean[j]) * rstd[j], w[j], b[j]);
+      activate<V>(a.activation, z);
+      store_out<TO, V>(y + p * a.ys_r, z, a.inv_y, k.valid);
+    }
+  }
+}
+
+// Sums of a part of the pixels.  A channel's mean and squares about it are carried along in each thread
+// (m += d / i, s += d d'), so that a mean far from zero costs no digits; the threads' are joined about the
+// group's mean.
+template <typename TI>
+__global__ __launch_bounds__(1024) void last_stats(NormArgs a) {
+  constexpr int V = kVec<TI>;
+  extern __shared__ float4 lds[];
+  const int id = blockIdx.x / a.chunks, chunk = blockIdx.x - id * a.chunks, n = id / a.slabs;
+  const Column<TI> k(a, n, id - n * a.slabs);
+  const int first = chunk * a.per, last = min(a.P, first + a.per);
+  const TI* x = static_cast<const TI*>(a.x) + n * a.xs_n + k.c;
+  const int64_t room = a.x_end - n * a.xs_n - k.c;
+  float m[V], s[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) m[j] = s[j] = 0.0f;
+  int count = 0;
+  if (k.valid) {
+    for (int p = first + k.row; p < last; p += 4 * k.rows) {
+      raw4 r[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int q = p + u * k.rows;
+        if (q < last) r[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (p + u * k.rows < last) {
+          const float step = __builtin_amdgcn_rcpf((float)++count);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float e = element<TI>(r[u], j), d = e - m[j];
+            m[j] = fmaf(d, step, m[j]);
+            s[j] = fmaf(d, e - m[j], s[j]);
+          }
+        }
+      }
+    }
+  }
+  int group[V];
+  groups_of<TI>(a, k, group);
+  float* means = reinterpret_cast<float*>(lds);
+  float* squares = means + a.slab;
+  float* rows = means + (2 * a.slab + 3) / 4 * 4;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = m[j] * (float)count;
+  slab_sums<V>(a, k.groups, v, rows, means);
+  const float pixels = (float)(last - first), inv = 1.0f / ((float)a.cpg * pixels);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float d = m[j] - means[group[j]] * inv;
+    v[j] = count ? fmaf(d * d, (float)count, s[j]) : 0.0f;
+  }
+  slab_sums<V>(a, k.groups, v, rows, squares);
+  for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
+    reinterpret_cast<float4*>(a.part)[((int64_t)n * a.G + k.g0 + g) * a.chunks + chunk] =
+        make_float4(means[g] * inv, squares[g], (float)a.cpg * pixels, 0.0f);
+}
+
+// Mean and 1 / sd of the slab's groups from their parts, into LDS.
+__device__ __forceinline__ void slab_stats(const NormArgs& a, int n, int g0, int groups, float2* stat) {
+  const int width = lanes_of(groups), lane = threadIdx.x & (width - 1);
+  for (int g = threadIdx.x / width; g < groups; g += (int)blockDim.x / width) {
+    const float2 s = combine_parts(a, n, g0 + g, lane, width);
+    if (lane == 0) stat[g] = s;
+  }
+  __syncthreads();
+}
+
+template <typename TI, typename TO>
+__global__ __launch_bounds__(1024) void last_apply(NormArgs a) {
+  constexpr int V = kVec<TI>;
+  extern __shared__ float4 lds[];
+  float2* stat = reinterpret_cast<float2*>(lds);
+  const int id = blockIdx.x / a.chunks, chunk = blockIdx.x - id * a.chunks, n = id / a.slabs;
+  const Column<TI> k(a, n, id - n * a.slabs);
+  const int first = chunk * a.per, last = min(a.P, first + a.per);
+  const TI* x = static_cast<const TI*>(a.x) + n * a.xs_n + k.c;
+  TO* y = static_cast<TO*>(a.y) + n * a.ys_n + k.c;
+  const int64_t room = a.x_end - n * a.xs_n - k.c;
+  slab_stats(a, n, k.g0, k.groups, stat);
+  if (chunk == 0)
+    for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
+      reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] = stat[g];
+  if (!k.valid) return;
+  float w[V], b[V], mean[V], rstd[V];
+  int group[V];
+  affine_of<TI>(a, k, w, b);
+  groups_of<TI>(a, k, group);
+#pragma unroll
+  for (int j = 0; j < V; ++j) mean[j] = stat[group[j]].x, rstd[j] = stat[group[j]].y;
+  for (int p = first + k.row; p < last; p += 4 * k.rows) {
+    raw4 r[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int q = p + u * k.rows;
+      if (q < last) r[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int q = p + u * k.rows;
+      if (q < last) {
+        float z[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) z[j] = fmaf((element<TI>(r[u], j) - mean[j]) * rstd[j], w[j], b[j]);
+        activate<V>(a.activation, z);
+        store_out<TO, V>(y + q * a.ys_r, z, a.inv_y, k.valid);
+      }
+    }
+  }
+}
+
+// ---- backward ----
+
+// h and dz of a vector.
+template <typename T>
+__device__ __forceinline__ void back_vector(const NormArgs& a, const raw4& x, const raw4& dy,
+                                            const float (&mean)[kVec<T>], const float (&rstd)[kVec<T>],
+                                            const float (&w)[kVec<T>], const float (&b)[kVec<T>],
+                                            float (&h)[kVec<T>], float (&dz)[kVec<T>]) {
+  constexpr int V = kVec<T>;
+  float z[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    h[j] = (element<T>(x, j) - mean[j]) * rstd[j];
+    z[j] = fmaf(h[j], w[j], b[j]);
+    dz[j] = element<T>(dy, j);
+  }
+  activate_back<V>(a.activation, z, dz);
+}
+
+// Sums of a part of the pixels: of each channel (part_c: dz, dz h) and of each group (part: w dz, w dz h).
+template <typename T>
+__global__ __launch_bounds__(1024) void last_back_sums(NormArgs a) {
+  constexpr int V = kVec<T>;
+  extern __shared__ float4 lds[];
+  const int id = blockIdx.x / a.chunks, chunk = blockIdx.x - id * a.chunks, n = id / a.slabs;
+  const Column<T> k(a, n, id - n * a.slabs);
+  const int first = chunk * a.per, last = min(a.P, first + a.per);
+  const T* x = static_cast<const T*>(a.x) + n * a.xs_n + k.c;
+  const T* dy = static_cast<const T*>(a.dy) + n * a.ys_n + k.c;
+  const int64_t room = a.x_end - n * a.xs_n - k.c, room_y = a.y_end - n * a.ys_n - k.c;
+  float w[V], b[V], mean[V], rstd[V], s1[V], s2[V];
+  int group[V];
+  affine_of<T>(a, k, w, b);
+  groups_of<T>(a, k, group);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 s = reinterpret_cast<const float2*>(a.stats)[(int64_t)n * a.G + k.g0 + group[j]];
+    mean[j] = s.x, rstd[j] = s.y;
+    s1[j] = s2[j] = 0.0f;
+  }
+  if (k.valid) {
+    for (int p = first + k.row; p < last; p += 2 * k.rows) {
+      raw4 rx[2], ry[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int q = p + u * k.rows;
+        if (q < last) {
+          rx[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
+          ry[u] = load_cut(dy + q * a.ys_r, k.valid, room_y - q * a.ys_r);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (p + u * k.rows < last) {
+          float h[V], dz[V];
+          back_vector<T>(a, rx[u], ry[u], mean, rstd, w, b, h, dz);
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            s1[j] += dz[j];
+            s2[j] = fmaf(dz[j], h[j], s2[j]);
+          }
+        }
+      }
+    }
+  }
+  // channels first, then the groups' sums of them
+  float* rows = reinterpret_cast<float*>(lds);
+  const int pitch = V << a.lanes;
+  const int slots = (1 << a.lanes) < 64 ? (int)blockDim.x >> 6 : (int)blockDim.x >> a.lanes;
+  float2* channels = reinterpret_cast<float2*>(rows + slots * pitch);
+  slab_rows<V>(a, s1, rows);
+  for (int c = threadIdx.x; c < k.width; c += (int)blockDim.x) {
+    float s = 0.0f;
+    for (int r = 0; r < slots; ++r) s += rows[r * pitch + c];
+    channels[c].x = s;
+  }
+  __syncthreads();
+  slab_rows<V>(a, s2, rows);
+  for (int c = threadIdx.x; c < k.width; c += (int)blockDim.x) {
+    float s = 0.0f;
+    for (int r = 0; r < slots; ++r) s += rows[r * pitch + c];
+    channels[c].y = s;
+    reinterpret_cast<float2*>(a.part_c)[n * a.c_image + chunk * a.c_chunk + k.g0 * a.cpg + c] =
+        make_float2(channels[c].x, s);
+  }
+  __syncthreads();
+  const int width = lanes_of(k.groups), lane = threadIdx.x & (width - 1);
+  for (int g = threadIdx.x / width; g < k.groups; g += (int)blockDim.x / width) {
+    float2 s = make_float2(0.0f, 0.0f);
+    for (int j = lane; j < a.cpg; j += width) {
+      const int c = g * a.cpg + j;
+      const float wc = a.weight ? a.weight[k.g0 * a.cpg + c] : 1.0f;
+      s.x += wc * channels[c].x, s.y += wc * channels[c].y;
+    }
+    for (int m = width >> 1; m; m >>= 1) s.x += __shfl_xor(s.x, m, 64), s.y += __shfl_xor(s.y, m, 64);
+    if (lane == 0) reinterpret_cast<float2*>(a.part)[((int64_t)n * a.G + k.g0 + g) * a.chunks + chunk] = s;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_dx(const float (&rstd)[kVec<T>], const float (&w)[kVec<T>],
+                                         const float (&c1)[kVec<T>], const float (&c2)[kVec<T>],
+                                         const float (&h)[kVec<T>], const float (&dz)[kVec<T>], T* dx, int valid) {
+// (the product is rounded before the difference, as in the sums: a group of one element gives exactly zero)
+#pragma clang fp contract(off)
+  constexpr int V = kVec<T>;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float d = dz[j] * w[j] - c1[j];
+    v[j] = rstd[j] * (d - h[j] * c2[j]);
+  }
+  store_vec<T, V>(dx, v, valid);
+}
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void last_back_apply(NormArgs a) {
+  constexpr int V = kVec<T>;
+  extern __shared__ float4 lds[];
+  if ((int)blockIdx.x < a.finals) {
+    channel_sums(a, blockIdx.x, reinterpret_cast<float2*>(lds));
+    return;
+  }
+  const int block = blockIdx.x - a.finals;
+  const int id = block / a.chunks, chunk = block - id * a.chunks, n = id / a.slabs;
+  const Column<T> k(a, n, id - n * a.slabs);
+  const int first = chunk * a.per, last = min(a.P, first + a.per);
+  const T* x = static_cast<const T*>(a.x) + n * a.xs_n + k.c;
+  const T* dy = static_cast<const T*>(a.dy) + n * a.ys_n + k.c;
+  T* dx = static_cast<T*>(a.y) + n * a.xs_n + k.c;
+  const int64_t room = a.x_end - n * a.xs_n - k.c, room_y = a.y_end - n * a.ys_n - k.c;
+  float2* means = reinterpret_cast<float2*>(lds);
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const int width = lanes_of(k.groups), lane = threadIdx.x & (width - 1);
+  for (int g = threadIdx.x / width; g < k.groups; g += (int)blockDim.x / width) {
+    const float2* part = reinterpret_cast<const float2*>(a.part) + ((int64_t)n * a.G + k.g0 + g) * a.chunks;
+    float2 s = make_float2(0.0f, 0.0f);
+    for (int i = lane; i < a.chunks; i += width) s.x += part[i].x, s.y += part[i].y;
+    for (int m = width >> 1; m; m >>= 1) s.x += __shfl_xor(s.x, m, 64), s.y += __shfl_xor(s.y, m, 64);
+    if (lane == 0) means[g] = make_float2(s.x * inv, s.y * inv);
+  }
+  __syncthreads();
+  if (!k.valid) return;
+  float w[V], b[V], mean[V], rstd[V], c1[V], c2[V];
+  int group[V];
+  affine_of<T>(a, k, w, b);
+  groups_of<T>(a, k, group);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 s = reinterpret_cast<const float2*>(a.stats)[(int64_t)n * a.G + k.g0 + group[j]];
+    mean[j] = s.x, rstd[j] = s.y;
+    c1[j] = means[group[j]].x, c2[j] = means[group[j]].y;
+  }
+  for (int p = first + k.row; p < last; p += 2 * k.rows) {
+    raw4 rx[2], ry[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int q = p + u * k.rows;
+      if (q < last) {
+        rx[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
+        ry[u] = load_cut(dy + q * a.ys_r, k.valid, room_y - q * a.ys_r);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int q = p + u * k.rows;
+      if (q < last) {
+        float h[V], dz[V];
+        back_vector<T>(a, rx[u], ry[u], mean, rstd, w, b, h, dz);
+        store_dx<T>(rstd, w, c1, c2, h, dz, dx + q * a.xs_r, k.valid);
+      }
+    }
+  }
+}
+
+int log2_up(int64_t n) {
+  int s = 0;
+  while (((int64_t)1 << s) < n) ++s;
+  return s;
+}
+
+void set_slab(NormArgs* a, int groups, int V) {
+  a->slab = groups < a->G ? groups : a->G;
+  a->slabs = (a->G + a->slab - 1) / a->slab;
+  a->lanes = log2_up(((int64_t)a->slab * a->cpg + V - 1) / V);
+  a->by_p = FastDiv::by((unsigned)a->cpg);  // channel of the slab -> group
+}
+
+// Two kernels: as many whole groups as 256 threads have vector columns for (a wider group has 1024), and parts
+// of the pixels for some 1024 workgroups, each of at least 16 rows of threads; the parts of one image stay few enough
+// for every workgroup of the second kernel to join them (4096 group parts: 64 KB out of the L2).
+void set_parts(NormArgs* a, int x_size) {
+  const int V = 16 / x_size;
+  a->threads = a->cpg > 256 * V ? 1024 : 256;
+  set_slab(a, a->cpg < 256 * V ? 256 * V / a->cpg : 1, V);
+  const int rows = a->threads >> a->lanes;
+  const int64_t cells = (int64_t)a->N * a->slabs;
+  int64_t parts = (1024 + cells - 1) / cells;
+  const int64_t most = a->P / (16 * rows) > 1 ? a->P / (16 * rows) : 1;
+  parts = parts < most ? parts : most;
+  const int64_t joined = 4096 / a->slab > 1 ? 4096 / a->slab : 1;
+  parts = parts < joined ? parts : joined;
+  a->per = (int)((a->P + parts - 1) / parts);
+  a->chunks = (a->P + a->per - 1) / a->per;
+  a->per_thread = 0;
+}
+
+unsigned rows_bytes(const NormArgs& a, int V) {
+  const int lanes = 1 << a.lanes, slots = lanes < 64 ? a.threads / 64 : a.threads / lanes;
+  return (unsigned)(slots * lanes * V) * 4u;
+}
+
+unsigned sums_bytes(const NormArgs& a, int V) { return (unsigned)((2 * a.slab + 3) / 4 * 16) + rows_bytes(a, V); }
+
+}  // namespace
+
+size_t plan_norm_last(NormArgs* a, int x_size, bool resident_allowed) {
+  const int V = 16 / x_size;
+  // one kernel: slabs of at least 128 bytes of a pixel, so that whole cache lines are read
+  const int wide = (128 / x_size + a->cpg - 1) / a->cpg;
+  set_slab(a, wide, V);
+  a->chunks = 1;
+  a->per = a->P;
+  for (int threads = 64; resident_allowed && threads <= 1024; threads *= 2) {
+    const int rows = threads >> a->lanes;
+    if (rows == 0) continue;
+    const int64_t each = ((int64_t)a->P + rows - 1) / rows;
+    if (each > (threads < 1024 ? 4 : 8)) continue;
+    a->threads = threads;
+    a->per_thread = each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
+    // (few slabs over long maps leave most of the chip idle)
+    if ((int64_t)a->N * a->slabs >= 128 || each * threads <= 2048) return 0;
+  }
+  set_parts(a, x_size);
+  return (size_t)a->N * a->G * a->chunks * 16;
+}
+
+size_t plan_norm_last_backward(NormArgs* a, int x_size) {
+  set_parts(a, x_size);
+  a->c_group = a->cpg;
+  a->c_chunk = a->C;
+  a->c_image = (int64_t)a->chunks * a->C;
+  return (size_t)a->N * a->chunks * ((size_t)a->C + a->G) * 8;
+}
+
+namespace {
+
+template <typename TI, typename TO>
+hipError_t run_last(const NormArgs& a, hipStream_t s) {
+  constexpr int V = kVec<TI>;
+  if (a.per_thread) {
+    const dim3 grid((unsigned)((int64_t)a.N * a.slabs)), block((unsigned)a.threads);
+    const unsigned bytes = sums_bytes(a, V);
+    switch (a.per_thread) {
+      case 1: last_resident<TI, TO, 1><<<grid, block, bytes, s>>>(a); break;
+      case 2: last_resident<TI, TO, 2><<<grid, block, bytes, s>>>(a); break;
+      case 4: last_resident<TI, TO, 4><<<grid, block, bytes, s>>>(a); break;
+      default: last_resident<TI, TO, 8><<<grid, block, bytes, s>>>(a); break;
+    }
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)((int64_t)a.N * a.slabs * a.chunks)), block((unsigned)a.threads);
+  last_stats<TI><<<grid, block, sums_bytes(a, V), s>>>(a);
+  last_apply<TI, TO><<<grid, block, (unsigned)a.slab * 8u, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_last_back(NormArgs a, hipStream_t s) {
+  constexpr int V = kVec<T>;
+  const unsigned cells = (unsigned)((int64_t)a.N * a.slabs * a.chunks);
+  const dim3 block((unsigned)a.threads);
+  last_back_sums<T><<<cells, block, rows_bytes(a, V) + (unsigned)(a.slab * a.cpg) * 8u, s>>>(a);
+  a.finals = a.dweight || a.dbias ? (a.C + 7) / 8 : 0;
+  const unsigned bytes = (unsigned)a.slab * 8u;
+  const dim3 grid(cells + (unsigned)a.finals);
+  // (registers for 256 threads where the slab allows it: with the 128 of a larger workgroup some would spill)
+  if (a.threads == 256) last_back_apply<T, 256><<<grid, block, bytes > 256u ? bytes : 256u, s>>>(a);
+  else last_back_apply<T, 1024><<<grid, block, bytes > 1024u ? bytes : 1024u, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_last(const NormArgs& a, int x_type, int y_type, hipStream_t s) {
+  if (x_type == kNormF32) {
+    if (y_type == kNormF32) return run_last<float, float>(a, s);
+    if (y_type == kNormF16) return run_last<float, f16>(a, s);
+    return run_last<float, bf16>(a, s);
+  }
+  return x_type == kNormF16 ? run_last<f16, f16>(a, s) : run_last<bf16, bf16>(a, s);
+}
+
+hipError_t launch_norm_last_stats(const NormArgs& a, int x_type, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.N * a.slabs * a.chunks)), block((unsigned)a.threads);
+  if (x_type == kNormF32) last_stats<float><<<grid, block, sums_bytes(a, 4), s>>>(a);
+  else if (x_type == kNormF16) last_stats<f16><<<grid, block, sums_bytes(a, 8), s>>>(a);
+  else last_stats<bf16><<<grid, block, sums_bytes(a, 8), s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_last_backward(const NormArgs& a, int x_type, hipStream_t s) {
+  if (x_type == kNormF32) return run_last_back<float>(a, s);
+  return x_type == kNormF16 ? run_last_back<f16>(a, s) : run_last_back<bf16>(a, s);
+}
+
+}  // namespace sfc

@@ -1,0 +1,623 @@
+// Group norm with an activation on planes (NCHW).
+//
+// A group of an image is cpg planes of P pixels.  Where the planes lie side by side they are one run of cpg P
+// elements, cut into vectors of 16 bytes whatever the pixel count is: a vector then holds elements of two channels
+// at most (P >= a vector's elements), the first `bound` of them of channel `ch`, the others of ch + 1.  Else (planes
+// with gaps, or of fewer pixels than a vector) every plane is a run of its own and its last vector is cut short.
+//
+// A group that fits the registers of a workgroup is read once (planes_resident, planes_back_resident): its vectors
+// stay as they were loaded between the sums and the result, so HBM carries each tensor once and the kernels are bound
+// by it.  Larger groups take two kernels: sums of parts, then the result from the joined sums; the second read comes
+// from the L2 and the memory-side cache as far as they reach.
+#include "sfc_norm.hpp"
+
+namespace sfc {
+namespace {
+
+struct Item {
+  int64_t at;              // offset from the group's first element
+  int valid, ch, bound;
+};
+
+template <typename T>
+__device__ __forceinline__ Item item_of(const NormArgs& a, int q, int64_t row_stride) {
+  constexpr int V = kVec<T>;
+  Item it;
+  if (a.segments == 1) {
+    const int e = q * V;
+    it.at = e;
+    it.valid = min(V, a.cpg * a.P - e);
+    it.ch = a.by_p(e);
+    it.bound = (it.ch + 1) * a.P - e;
+  } else {
+    const int seg = a.by_vps(q), e = (q - seg * a.vps) * V;
+    it.at = seg * row_stride + e;
+    it.valid = min(V, a.P - e);
+    it.ch = seg;
+    it.bound = V;
+  }
+  return it;
+}
+
+// Weights and biases of the group's channels, in LDS; one entry more, for the vector that ends the group.
+__device__ __forceinline__ void stage_affine(const NormArgs& a, int g, float2* wb) {
+  for (int c = threadIdx.x; c <= a.cpg; c += blockDim.x) {
+    const int at = g * a.cpg + min(c, a.cpg - 1);
+    wb[c] = make_float2(a.weight ? a.weight[at] : 1.0f, a.bias ? a.bias[at] : 0.0f);
+  }
+}
+
+template <typename TI, typename TO>
+__device__ __forceinline__ void finish_item(const NormArgs& a, const Item& it, const raw4& raw, float2 stat,
+                                            const float2* wb, TO* y) {
+  constexpr int V = kVec<TI>;
+  const float2 w0 = wb[it.ch], w1 = wb[it.ch + 1];
+  float z[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 w = j < it.bound ? w0 : w1;
+    z[j] = fmaf((element<TI>(raw, j) - stat.x) * stat.y, w.x, w.y);
+  }
+  activate<V>(a.activation, z);
+  store_out<TO, V>(y, z, a.inv_y, it.valid);
+}
+
+template <typename TI, typename TO, int NV>
+__global__ __launch_bounds__(1024) void planes_resident(NormArgs a) {
+  constexpr int V = kVec<TI>;
+  extern __shared__ float2 lds[];
+  float* scratch = reinterpret_cast<float*>(lds + a.cpg + 1);
+  const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G, t = threadIdx.x;
+  const int items = a.segments * a.vps;
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r, y0 = n * a.ys_n + (int64_t)g * a.cpg * a.ys_r;
+  const TI* x = static_cast<const TI*>(a.x) + x0;
+  raw4 raw[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * (int)blockDim.x;
+    raw[u] = raw4{0u, 0u, 0u, 0u};
+    if (q < items) {
+      const Item it = item_of<TI>(a, q, a.xs_r);
+      raw[u] = load_cut(x + it.at, it.valid, a.x_end - x0 - it.at);
+    }
+  }
+  stage_affine(a, g, lds);
+  float sum = 0.0f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+#pragma unroll
+    for (int j = 0; j < V; ++j) sum += element<TI>(raw[u], j);
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float mean = block_sum(sum, scratch) * inv;
+  float squares = 0.0f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * (int)blockDim.x;
+    const int valid = q < items ? item_of<TI>(a, q, a.xs_r).valid : 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = element<TI>(raw[u], j) - mean;
+      squares += j < valid ? d * d : 0.0f;
+    }
+  }
+  const float var = block_sum(squares, scratch + 16) * inv;
+  const float2 stat = make_float2(mean, 1.0f / sqrtf(var + a.eps));
+  if (t == 0) reinterpret_cast<float2*>(a.stats)[blockIdx.x] = stat;
+  TO* y = static_cast<TO*>(a.y) + y0;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * (int)blockDim.x;
+    if (q < items) {
+      const Item it = item_of<TI>(a, q, a.xs_r);
+      const int64_t at = a.segments == 1 ? it.at : it.at + it.ch * (a.ys_r - a.xs_r);
+      finish_item<TI, TO>(a, it, raw[u], stat, lds, y + at);
+    }
+  }
+}
+
+// Sums of a part of a group, about the mean of its first vectors.
+template <typename TI>
+__global__ __launch_bounds__(256) void planes_stats(NormArgs a) {
+  constexpr int V = kVec<TI>;
+  __shared__ float scratch[16];
+  const int64_t ng = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x - (int)ng * a.chunks, n = (int)(ng / a.G), g = (int)(ng - (int64_t)n * a.G);
+  const int items = a.segments * a.vps, first = chunk * a.per, last = min(items, first + a.per);
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r;
+  const TI* x = static_cast<const TI*>(a.x) + x0;
+  auto load = [&](int q, int* valid) {
+    *valid = 0;
+    if (q >= last) return raw4{0u, 0u, 0u, 0u};
+    const Item it = item_of<TI>(a, q, a.xs_r);
+    *valid = it.valid;
+    return load_cut(x + it.at, it.valid, a.x_end - x0 - it.at);
+  };
+  const int t = threadIdx.x;
+  int valid;
+  const raw4 head = load(first + t, &valid);
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum += element<TI>(head, j);
+  const float about = block_sum(sum, scratch) / block_sum((float)valid, scratch + 4);
+  float s = 0.0f, ss = 0.0f, count = 0.0f;
+  auto add = [&](const raw4& r, int valid) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const float d = j < valid ? element<TI>(r, j) - about : 0.0f;
+      s += d;
+      ss = fmaf(d, d, ss);
+    }
+    count += (float)valid;
+  };
+  add(head, valid);
+  for (int q = first + t + 256; q < last; q += 1024) {
+    raw4 r[4];
+    int v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) r[k] = load(q + 256 * k, &v[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) add(r[k], v[k]);
+  }
+  s = block_sum(s, scratch + 8);
+  ss = block_sum(ss, scratch + 12);
+  __syncthreads();
+  count = block_sum(count, scratch);
+  if (t == 0) {
+    const float d = s / count;
+    reinterpret_cast<float4*>(a.part)[ng * a.chunks + chunk] =
+        make_float4(about + d, fmaxf(ss - s * d, 0.0f * ss), count, 0.0f);
+  }
+}
+
+template <typename TI, typename TO>
+__global__ __launch_bounds__(256) void planes_apply(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const int64_t ng = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x - (int)ng * a.chunks, n = (int)(ng / a.G), g = (int)(ng - (int64_t)n * a.G);
+  const int items = a.segments * a.vps, first = chunk * a.per, last = min(items, first + a.per);
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r, y0 = n * a.ys_n + (int64_t)g * a.cpg * a.ys_r;
+  const TI* x = static_cast<const TI*>(a.x) + x0;
+  TO* y = static_cast<TO*>(a.y) + y0;
+  stage_affine(a, g, lds);
+  const float2 stat = combine_parts(a, n, g, threadIdx.x & 63, 64);
+  if (chunk == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.stats)[ng] = stat;
+  __syncthreads();
+  for (int q = first + threadIdx.x; q < last; q += 1024) {
+    raw4 r[4];
+    Item it[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (q + 256 * k < last) {
+        it[k] = item_of<TI>(a, q + 256 * k, a.xs_r);
+        r[k] = load_cut(x + it[k].at, it[k].valid, a.x_end - x0 - it[k].at);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (q + 256 * k < last) {
+        const int64_t at = a.segments == 1 ? it[k].at : it[k].at + it[k].ch * (a.ys_r - a.xs_r);
+        finish_item<TI, TO>(a, it[k], r[k], stat, lds, y + at);
+      }
+    }
+  }
+}
+
+// ---- backward ----
+
+// h and dz of a vector; elements past `valid` give dz = 0.
+template <typename T>
+__device__ __forceinline__ void back_item(const NormArgs& a, const Item& it, const raw4& x, const raw4& dy,
+                                          float2 stat, const float2* wb, float (&h)[kVec<T>],
+                                          float (&dz)[kVec<T>]) {
+  constexpr int V = kVec<T>;
+  const float2 w0 = wb[it.ch], w1 = wb[it.ch + 1];
+  float z[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 w = j < it.bound ? w0 : w1;
+    h[j] = (element<T>(x, j) - stat.x) * stat.y;
+    z[j] = fmaf(h[j], w.x, w.y);
+    dz[j] = element<T>(dy, j);
+  }
+  activate_back<V>(a.activation, z, dz);
+}
+
+// dx = rstd (w dz - c1 - h c2), c1 and c2 the group's means of w dz and w dz h.  The product is rounded before the
+// difference, as in the sums: a group of one element then gives exactly zero.
+template <typename T>
+__device__ __forceinline__ void store_dx(const Item& it, float2 stat, float c1, float c2, const float2* wb,
+                                         const float (&h)[kVec<T>], const float (&dz)[kVec<T>], T* dx) {
+#pragma clang fp contract(off)
+  constexpr int V = kVec<T>;
+  const float w0 = wb[it.ch].x, w1 = wb[it.ch + 1].x;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float d = dz[j] * (j < it.bound ? w0 : w1) - c1;
+    v[j] = stat.y * (d - h[j] * c2);
+  }
+  store_vec<T, V>(dx, v, it.valid);
+}
+
+// Sums of a vector's two channels: (dz, dz h) of ch in `head`, of ch + 1 in `next`.
+template <typename T>
+__device__ __forceinline__ void item_sums(const Item& it, const float (&h)[kVec<T>], const float (&dz)[kVec<T>],
+                                          float2* head, float2* next) {
+  float2 p = make_float2(0.0f, 0.0f), q = p;
+#pragma unroll
+  for (int j = 0; j < kVec<T>; ++j) {
+    const float e = dz[j] * h[j];
+    if (j < it.bound) p.x += dz[j], p.y += e;
+    else if (j < it.valid) q.x += dz[j], q.y += e;
+  }
+  *head = p;
+  if (next) *next = q;
+}
+
+// The sums of channel c over the vectors [first, last) of the group, left in LDS by item_sums, by `width`
+// neighbouring lanes.
+template <typename T>
+__device__ __forceinline__ float2 channel_of_items(const NormArgs& a, int c, int first, int last,
+                                                   const float2* head, const float2* next, int lane, int width) {
+  constexpr int V = kVec<T>;
+  int q0, q1;
+  if (a.segments == 1) {
+    q0 = (c * a.P) / V, q1 = ((c + 1) * a.P + V - 1) / V;
+  } else {
+    q0 = c * a.vps, q1 = q0 + a.vps;
+  }
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int q = max(q0, first) + lane; q < min(q1, last); q += width) {
+    const bool straddles = a.segments == 1 && q * V < c * a.P;
+    const float2 v = straddles ? next[q - first] : head[q - first];
+    s.x += v.x, s.y += v.y;
+  }
+  for (int m = width >> 1; m; m >>= 1) s.x += __shfl_xor(s.x, m, 64), s.y += __shfl_xor(s.y, m, 64);
+  return s;
+}
+
+// Sums over a group's channels of w dz and w dz h, in every lane of every wave.
+__device__ __forceinline__ float2 group_of_channels(const NormArgs& a, const float2* channels, const float2* wb) {
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int c = threadIdx.x & 63; c < a.cpg; c += 64) {
+    s.x += wb[c].x * channels[c].x;
+    s.y += wb[c].x * channels[c].y;
+  }
+  return make_float2(wave_sum(s.x), wave_sum(s.y));
+}
+
+// Lanes that add a channel: as many as give every channel its own, no more than a wave.
+__device__ __forceinline__ int lanes_of(int channels, int threads) {
+  int width = 64;
+  while (width > 1 && channels * width > threads) width >>= 1;
+  return width;
+}
+
+template <typename T, int NV>
+__global__ __launch_bounds__(1024) void planes_back_resident(NormArgs a) {
+  extern __shared__ float2 lds[];
+  const int items = a.segments * a.vps;
+  float2* wb = lds;
+  float2* channels = wb + a.cpg + 1;
+  float2* head = channels + a.cpg;
+  float2* next = a.segments == 1 ? head + items : nullptr;
+  const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G, t = threadIdx.x, threads = blockDim.x;
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r, y0 = n * a.ys_n + (int64_t)g * a.cpg * a.ys_r;
+  const T* x = static_cast<const T*>(a.x) + x0;
+  const T* dy = static_cast<const T*>(a.dy) + y0;
+  T* dx = static_cast<T*>(a.y) + x0;
+  raw4 rx[NV], ry[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * threads;
+    if (q < items) {
+      const Item it = item_of<T>(a, q, a.xs_r);
+      const int64_t at = a.segments == 1 ? it.at : it.at + it.ch * (a.ys_r - a.xs_r);
+      rx[u] = load_cut(x + it.at, it.valid, a.x_end - x0 - it.at);
+      ry[u] = load_cut(dy + at, it.valid, a.y_end - y0 - at);
+    }
+  }
+  stage_affine(a, g, wb);
+  const float2 stat = reinterpret_cast<const float2*>(a.stats)[blockIdx.x];
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * threads;
+    if (q < items) {
+      const Item it = item_of<T>(a, q, a.xs_r);
+      float h[kVec<T>], dz[kVec<T>];
+      back_item<T>(a, it, rx[u], ry[u], stat, wb, h, dz);
+      item_sums<T>(it, h, dz, head + q, next ? next + q : nullptr);
+    }
+  }
+  __syncthreads();
+  const int width = lanes_of(a.cpg, threads), lane = t & (width - 1);
+  for (int c = t / width; c < a.cpg; c += threads / width) {
+    const float2 s = channel_of_items<T>(a, c, 0, items, head, next, lane, width);
+    if (lane == 0) {
+      channels[c] = s;
+      reinterpret_cast<float2*>(a.part_c)[(int64_t)blockIdx.x * a.cpg + c] = s;
+    }
+  }
+  __syncthreads();
+  const float2 sums = group_of_channels(a, channels, wb);
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float c1 = sums.x * inv, c2 = sums.y * inv;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    const int q = t + u * threads;
+    if (q < items) {
+      const Item it = item_of<T>(a, q, a.xs_r);
+      float h[kVec<T>], dz[kVec<T>];
+      back_item<T>(a, it, rx[u], ry[u], stat, wb, h, dz);
+      store_dx<T>(it, stat, c1, c2, wb, h, dz, dx + it.at);
+    }
+  }
+}
+
+constexpr int kBackItems = 1024;  // vectors whose sums lie in LDS at a time (planes_back_sums)
+
+// Sums of a part of a group: of its channels (part_c) and of the group (part).
+template <typename T>
+__global__ __launch_bounds__(256) void planes_back_sums(NormArgs a) {
+  extern __shared__ float2 lds[];
+  float2* wb = lds;
+  float2* channels = wb + a.cpg + 1;
+  float2* head = channels + a.cpg;
+  float2* next = a.segments == 1 ? head + kBackItems : nullptr;
+  const int64_t ng = blockIdx.x / a.chunks;
+  const int chunk = blockIdx.x - (int)ng * a.chunks, n = (int)(ng / a.G), g = (int)(ng - (int64_t)n * a.G);
+  const int t = threadIdx.x;
+  const int items = a.segments * a.vps, first = chunk * a.per, last = min(items, first + a.per);
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r, y0 = n * a.ys_n + (int64_t)g * a.cpg * a.ys_r;
+  const T* x = static_cast<const T*>(a.x) + x0;
+  const T* dy = static_cast<const T*>(a.dy) + y0;
+  stage_affine(a, g, wb);
+  for (int c = t; c < a.cpg; c += 256) channels[c] = make_float2(0.0f, 0.0f);
+  const float2 stat = reinterpret_cast<const float2*>(a.stats)[ng];
+  __syncthreads();
+  for (int q0 = first; q0 < last; q0 += kBackItems) {
+    const int q1 = min(last, q0 + kBackItems);
+    raw4 rx[kBackItems / 256], ry[kBackItems / 256];
+#pragma unroll
+    for (int u = 0; u < kBackItems / 256; ++u) {
+      const int q = q0 + t + u * 256;
+      if (q < q1) {
+        const Item it = item_of<T>(a, q, a.xs_r);
+        const int64_t at = a.segments == 1 ? it.at : it.at + it.ch * (a.ys_r - a.xs_r);
+        rx[u] = load_cut(x + it.at, it.valid, a.x_end - x0 - it.at);
+        ry[u] = load_cut(dy + at, it.valid, a.y_end - y0 - at);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kBackItems / 256; ++u) {
+      const int q = q0 + t + u * 256;
+      if (q < q1) {
+        const Item it = item_of<T>(a, q, a.xs_r);
+        float h[kVec<T>], dz[kVec<T>];
+        back_item<T>(a, it, rx[u], ry[u], stat, wb, h, dz);
+        item_sums<T>(it, h, dz, head + (q - q0), next ? next + (q - q0) : nullptr);
+      }
+    }
+    __syncthreads();
+    const Item begin = item_of<T>(a, q0, a.xs_r), end = item_of<T>(a, q1 - 1, a.xs_r);
+    const int c0 = begin.ch, c1 = min(a.cpg, end.ch + 1 + (end.bound < end.valid ? 1 : 0));
+    const int width = lanes_of(c1 - c0, 256), lane = t & (width - 1);
+    for (int c = c0 + t / width; c < c1; c += 256 / width) {
+      const float2 s = channel_of_items<T>(a, c, q0, q1, head, next, lane, width);
+      if (lane == 0) channels[c].x += s.x, channels[c].y += s.y;
+    }
+    __syncthreads();
+  }
+  for (int c = t; c < a.cpg; c += 256)
+    reinterpret_cast<float2*>(a.part_c)[(ng * a.chunks + chunk) * a.cpg + c] = channels[c];
+  const float2 s = group_of_channels(a, channels, wb);
+  if (t == 0) reinterpret_cast<float2*>(a.part)[ng * a.chunks + chunk] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void planes_back_apply(NormArgs a) {
+  extern __shared__ float2 lds[];
+  if ((int)blockIdx.x < a.finals) {
+    channel_sums(a, blockIdx.x, lds);
+    return;
+  }
+  const int64_t id = blockIdx.x - a.finals, ng = id / a.chunks;
+  const int chunk = (int)(id - ng * a.chunks), n = (int)(ng / a.G), g = (int)(ng - (int64_t)n * a.G);
+  const int items = a.segments * a.vps, first = chunk * a.per, last = min(items, first + a.per);
+  const int64_t x0 = n * a.xs_n + (int64_t)g * a.cpg * a.xs_r, y0 = n * a.ys_n + (int64_t)g * a.cpg * a.ys_r;
+  const T* x = static_cast<const T*>(a.x) + x0;
+  const T* dy = static_cast<const T*>(a.dy) + y0;
+  T* dx = static_cast<T*>(a.y) + x0;
+  stage_affine(a, g, lds);
+  const float2 stat = reinterpret_cast<const float2*>(a.stats)[ng];
+  float2 s = make_float2(0.0f, 0.0f);
+  for (int i = threadIdx.x & 63; i < a.chunks; i += 64) {
+    const float2 v = reinterpret_cast<const float2*>(a.part)[ng * a.chunks + i];
+    s.x += v.x, s.y += v.y;
+  }
+  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float c1 = wave_sum(s.x) * inv, c2 = wave_sum(s.y) * inv;
+  __syncthreads();
+  for (int q = first + threadIdx.x; q < last; q += 512) {
+    raw4 rx[2], ry[2];
+    Item it[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (q + 256 * k < last) {
+        it[k] = item_of<T>(a, q + 256 * k, a.xs_r);
+        const int64_t at = a.segments == 1 ? it[k].at : it[k].at + it[k].ch * (a.ys_r - a.xs_r);
+        rx[k] = load_cut(x + it[k].at, it[k].valid, a.x_end - x0 - it[k].at);
+        ry[k] = load_cut(dy + at, it[k].valid, a.y_end - y0 - at);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (q + 256 * k < last) {
+        float h[kVec<T>], dz[kVec<T>];
+        back_item<T>(a, it[k], rx[k], ry[k], stat, lds, h, dz);
+        store_dx<T>(it[k], stat, c1, c2, lds, h, dz, dx + it[k].at);
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void planes_back_finals(NormArgs a) {
+  extern __shared__ float2 lds[];
+  channel_sums(a, blockIdx.x, lds);
+}
+
+// Vectors of a group, and how its planes are cut into them.
+void cut_into_vectors(NormArgs* a, int x_size, bool dense) {
+  const int V = 16 / x_size;
+  const bool run = dense && a->P >= V;
+  const int64_t length = run ? (int64_t)a->cpg * a->P : a->P;
+  a->segments = run ? 1 : a->cpg;
+  a->vps = (int)((length + V - 1) / V);
+  a->by_vps = FastDiv::by((unsigned)a->vps);
+  a->by_p = FastDiv::by((unsigned)a->P);
+}
+
+// Workgroup and vectors of a thread for `items` vectors of which a thread keeps at most `most`; 0: they do not fit.
+void choose_resident(NormArgs* a, int64_t items, int most) {
+  a->threads = a->per_thread = 0;
+  for (int threads = 64; threads <= 1024; threads *= 2) {
+    // (a thread with up to four vectors before the workgroup grows)
+    if (items <= (int64_t)threads * (threads < 1024 ? 4 : most)) {
+      a->threads = threads;
+      int nv = 1;
+      while ((int64_t)nv * threads < items) nv *= 2;
+      a->per_thread = nv;
+      return;
+    }
+  }
+}
+
+// Parts of a group: some 2048 workgroups over the chip, none under 1024 vectors.
+void choose_parts(NormArgs* a, int64_t items) {
+  const int64_t groups = (int64_t)a->N * a->G;
+  int64_t parts = (2048 + groups - 1) / groups;
+  parts = parts < (items + 1023) / 1024 ? parts : (items + 1023) / 1024;
+  a->per = (int)((items + parts - 1) / parts + 255) / 256 * 256;
+  a->chunks = (int)((items + a->per - 1) / a->per);
+}
+
+}  // namespace
+
+size_t plan_norm_planes(NormArgs* a, int x_size, bool resident_allowed) {
+  cut_into_vectors(a, x_size, a->xs_r == a->P && a->ys_r == a->P);
+  const int64_t items = (int64_t)a->segments * a->vps;
+  choose_resident(a, items, 8);
+  // A group a workgroup, unless there are so few that most of the chip would idle over long groups.
+  if (!resident_allowed || ((int64_t)a->N * a->G < 128 && items > 2048)) a->threads = 0;
+  a->chunks = 1;
+  if (a->threads) return 0;
+  choose_parts(a, items);
+  return (size_t)a->N * a->G * a->chunks * 16;
+}
+
+size_t plan_norm_planes_backward(NormArgs* a, int x_size) {
+  cut_into_vectors(a, x_size, a->xs_r == a->P && a->ys_r == a->P);
+  const int64_t items = (int64_t)a->segments * a->vps;
+  choose_resident(a, items, 4);
+  if ((int64_t)a->N * a->G < 128 && items > 1024) a->threads = 0;
+  a->chunks = 1;
+  if (!a->threads) choose_parts(a, items);
+  const int64_t cells = (int64_t)a->N * a->G * a->chunks;
+  a->c_chunk = a->cpg;
+  a->c_group = (int64_t)a->chunks * a->cpg;
+  a->c_image = a->c_group * a->G;
+  return (size_t)(cells * a->cpg * 8 + (a->threads ? 0 : cells * 8));
+}
+
+namespace {
+
+template <typename TI, typename TO>
+hipError_t run_planes(const NormArgs& a, hipStream_t s) {
+  const int64_t groups = (int64_t)a.N * a.G;
+  const unsigned affine = (unsigned)(a.cpg + 1) * 8u;
+  if (a.threads) {
+    const dim3 grid((unsigned)groups), block((unsigned)a.threads);
+    const unsigned bytes = affine + 128u;
+    switch (a.per_thread) {
+      case 1: planes_resident<TI, TO, 1><<<grid, block, bytes, s>>>(a); break;
+      case 2: planes_resident<TI, TO, 2><<<grid, block, bytes, s>>>(a); break;
+      case 4: planes_resident<TI, TO, 4><<<grid, block, bytes, s>>>(a); break;
+      default: planes_resident<TI, TO, 8><<<grid, block, bytes, s>>>(a); break;
+    }
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)(groups * a.chunks));
+  planes_stats<TI><<<grid, 256, 0, s>>>(a);
+  planes_apply<TI, TO><<<grid, 256, affine, s>>>(a);
+  return hipGetLastError();
+}
+
+// More than 64 KB of dynamic LDS has to be asked for.
+template <typename K>
+hipError_t allow_lds(K kernel, unsigned bytes) {
+  if (bytes <= 65536u) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)bytes);
+}
+
+template <typename T, int NV>
+hipError_t run_back_resident(const NormArgs& a, dim3 grid, dim3 block, unsigned bytes, hipStream_t s) {
+  const hipError_t e = allow_lds(planes_back_resident<T, NV>, bytes);
+  if (e != hipSuccess) return e;
+  planes_back_resident<T, NV><<<grid, block, bytes, s>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_planes_back(NormArgs a, hipStream_t s) {
+  const int64_t groups = (int64_t)a.N * a.G;
+  const unsigned affine = (unsigned)(a.cpg + 1) * 8u, finals = (unsigned)(a.C + 7) / 8u;
+  const int sets = a.segments == 1 ? 2 : 1;  // sums of a vector's second channel
+  if (a.threads) {
+    const dim3 grid((unsigned)groups), block((unsigned)a.threads);
+    const unsigned bytes = affine + (unsigned)(a.cpg + sets * a.segments * a.vps) * 8u;
+    const hipError_t e = a.per_thread == 1   ? run_back_resident<T, 1>(a, grid, block, bytes, s)
+                         : a.per_thread == 2 ? run_back_resident<T, 2>(a, grid, block, bytes, s)
+                                             : run_back_resident<T, 4>(a, grid, block, bytes, s);
+    if (e != hipSuccess) return e;
+    if (a.dweight || a.dbias) planes_back_finals<<<finals, 256, 32 * 8, s>>>(a);
+    return hipGetLastError();
+  }
+  const unsigned cells = (unsigned)(groups * a.chunks);
+  const unsigned bytes = affine + (unsigned)(a.cpg + sets * kBackItems) * 8u;
+  const hipError_t e = allow_lds(planes_back_sums<T>, bytes);
+  if (e != hipSuccess) return e;
+  planes_back_sums<T><<<cells, 256, bytes, s>>>(a);
+  a.finals = a.dweight || a.dbias ? (int)finals : 0;
+  planes_back_apply<T><<<cells + (unsigned)a.finals, 256, affine > 256u ? affine : 256u, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm_planes(const NormArgs& a, int x_type, int y_type, hipStream_t s) {
+  if (x_type == kNormF32) {
+    if (y_type == kNormF32) return run_planes<float, float>(a, s);
+    if (y_type == kNormF16) return run_planes<float, f16>(a, s);
+    if (y_type == kNormBF16) return run_planes<float, bf16>(a, s);
+    return run_planes<float, int8_t>(a, s);
+  }
+  if (x_type == kNormF16) return y_type == kNormI8 ? run_planes<f16, int8_t>(a, s) : run_planes<f16, f16>(a, s);
+  return y_type == kNormI8 ? run_planes<bf16, int8_t>(a, s) : run_planes<bf16, bf16>(a, s);
+}
+
+hipError_t launch_norm_planes_stats(const NormArgs& a, int x_type, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.N * a.G * a.chunks));
+  if (x_type == kNormF32) planes_stats<float><<<grid, 256, 0, s>>>(a);
+  else if (x_type == kNormF16) planes_stats<f16><<<grid, 256, 0, s>>>(a);
+  else planes_stats<bf16><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_planes_backward(const NormArgs& a, int x_type, hipStream_t s) {
+  if (x_type == kNormF32) return run_planes_back<float>(a, s);
+  return x_type == kNormF16 ? run_planes_back<f16>(a, s) : run_planes_back<bf16>(a, s);
+}
+
+}  // namespace sfc

@@ -1,0 +1,392 @@
+"""Group norm with an activation against its definition in 64 bits: shapes that fill no vector, both layouts,
+strides, all types, int8 hand-over, gradients (formula and differences), refusals.
+
+Tolerances, set before the first run.  u = 2^-24 is the rounding of 32-bit arithmetic.  A normalized value
+carries a few roundings of x / sd (4 u max|x| / sd) and of itself; weight, activation and their sums add
+some ten more: 1e-5 of the largest output, plus that.  16-bit outputs add half a step of their type.
+Gradients are bounded alike with the sums of the magnitudes they are made of."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+U = 2.0 ** -24
+STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+ACTIVATIONS = ["none", "relu", "silu", "gelu"]
+# N, C, H, W, groups
+SHAPES = [
+    (1, 8, 1, 1, 4),  # two values to a group
+    (1, 4, 1, 1, 4),  # one value to a group: variance zero
+    (2, 6, 3, 5, 3),
+    (3, 46, 7, 9, 2),  # 23 channels to a group
+    (1, 512, 7, 7, 32),  # one image's deepest map
+    (5, 40, 17, 1, 8),
+    (1, 5, 1, 37, 5),  # a channel to a group
+    (2, 64, 56, 56, 32),
+    (70, 12, 5, 5, 3),
+    (1, 24, 131, 127, 1),  # one long group: the sums of parts
+    (2, 4096, 2, 3, 1),  # the widest group
+    (1, 16, 200, 203, 8),
+    (9, 184, 31, 45, 8),
+    (3, 32, 2, 2, 32),
+]
+
+
+def reference(x, groups, weight, bias, eps, activation):
+    """(y, h, z) in 64 bits."""
+    n, c = x.shape[:2]
+    v = x.double().contiguous().view(n, groups, -1)
+    mean = v.mean(2, keepdim=True)
+    var = ((v - mean) ** 2).mean(2, keepdim=True)
+    h = ((v - mean) / torch.sqrt(var + eps)).view(x.shape)
+    w = torch.ones(c).double() if weight is None else weight.double().cpu()
+    b = torch.zeros(c).double() if bias is None else bias.double().cpu()
+    z = h * w.to(x.device).view(1, -1, 1, 1) + b.to(x.device).view(1, -1, 1, 1)
+    y = {"none": lambda: z, "relu": lambda: z.clamp(min=0), "silu": lambda: z * torch.sigmoid(z),
+         "gelu": lambda: z * 0.5 * torch.special.erfc(-z / math.sqrt(2))}[activation]()
+    return y, h, z
+
+
+def spread(x, groups, eps):
+    """max |x| / sd of the worst group: what a value's own rounding is worth after normalization."""
+    v = x.double().contiguous().view(x.shape[0], groups, -1)
+    sd = torch.sqrt(v.var(2, unbiased=False) + eps)
+    return float((v.abs().amax(2) / sd).max())
+
+
+def make(shape, dtype, layout, seed=0, shift=0.0):
+    g = torch.Generator().manual_seed(seed)
+    n, c, h, w, _ = shape
+    x = torch.randn(n, c, h, w, generator=g) * (torch.rand(c, generator=g).view(1, -1, 1, 1) + 0.5) + shift
+    x = x + torch.randn(c, generator=g).view(1, -1, 1, 1)
+    weight, bias = torch.randn(c, generator=g) * 0.3 + 1, torch.randn(c, generator=g) * 0.3
+    dy = torch.randn(n, c, h, w, generator=g)
+    order = torch.channels_last if layout == "nhwc" else torch.contiguous_format
+    to = lambda t: t.to(dtype).cuda().contiguous(memory_format=order)  # noqa: E731
+    return to(x), weight.cuda(), bias.cuda(), to(dy)
+
+
+def bound(y, x, groups, eps, dtype):
+    top = float(y.abs().max())
+    return (1e-5 + 8 * U * spread(x, groups, eps)) * max(1.0, top) + STEP[dtype] * y.abs() + 2.0 ** -25
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_forward_and_backward(shape, layout, dtype):
+    from paper_2407_02913_amd import adapt
+
+    groups, eps = shape[4], 1e-5
+    for k, activation in enumerate(ACTIVATIONS):
+        x, weight, bias, dy = make(shape, dtype, layout, seed=k)
+        if k == 3:
+            weight = None
+        if k == 2:
+            bias = None
+        print("norm", shape, layout, dtype, activation, flush=True)
+        y, stats = adapt.group_norm_forward(x, groups, weight, bias, eps, activation)
+        ref, h, z = reference(x, groups, weight, bias, eps, activation)
+        assert y.dtype == dtype and y.stride() == x.stride()
+        assert ((y.double() - ref).abs() <= bound(ref, x, groups, eps, dtype)).all()
+        v = x.double().contiguous().view(x.shape[0], groups, -1)
+        sd = torch.sqrt(v.var(2, unbiased=False) + eps)
+        assert ((stats[..., 0] - v.mean(2)).abs() <= 64 * U * v.abs().amax(2)).all()
+        assert ((stats[..., 1] * sd - 1).abs() <= 1e-5 + 8 * U * spread(x, groups, eps) ** 2).all()
+        # the gradient from the definition
+        zz = z.detach().requires_grad_(True)
+        act = {"none": lambda t: t, "relu": torch.relu, "silu": torch.nn.functional.silu,
+               "gelu": torch.nn.functional.gelu}[activation](zz)
+        dz, = torch.autograd.grad(act, zz, dy.double())
+        w = torch.ones(x.shape[1], device="cuda").double() if weight is None else weight.double()
+        u = dz * w.view(1, -1, 1, 1)
+        ug, hg = (t.contiguous().view(x.shape[0], groups, -1) for t in (u, h))
+        c1, c2 = ug.mean(2, keepdim=True), (ug * hg).mean(2, keepdim=True)
+        dx_ref = ((ug - c1 - hg * c2) / sd.unsqueeze(2)).view(x.shape)
+        dx, dw, db = adapt.group_norm_backward(dy, x, stats, groups, weight, bias, eps, activation)
+        assert dx.dtype == dtype and dx.stride() == x.stride()
+        # what dx is made of, before its terms cancel; a relu's corner moves with z's own rounding
+        s = spread(x, groups, eps)
+        near = 1e-5 + 8 * U * s
+        terms = ((ug.abs() + c1.abs() + (hg * c2).abs()).amax(2, keepdim=True) / sd.unsqueeze(2)).expand_as(hg)
+        corner = 0.0
+        if activation == "relu":
+            flips = z.abs() <= near * max(1.0, float(z.abs().max()))
+            corner = float((flips * dy.double().abs()).sum() * w.abs().max() / sd.min() * (1 + h.abs().max() ** 2))
+        tol = near * 4 * (1 + float(h.abs().max())) * terms.reshape(x.shape) + STEP[dtype] * dx_ref.abs() + corner + 2.0 ** -25
+        assert ((dx.double() - dx_ref).abs() <= tol).all()
+        axes = (0, 2, 3)
+        big = 1 + float(h.abs().max())
+        assert ((db - dz.sum(axes)).abs() <= near * 4 * big * dy.double().abs().sum(axes) + corner).all()
+        assert ((dw - (dz * h).sum(axes)).abs() <= near * 4 * big * (dy.double() * h).abs().sum(axes)
+                + near * dy.double().abs().sum(axes) + corner * big).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1, 8, 1, 1, 4), (3, 46, 7, 9, 2), (2, 64, 14, 14, 32), (1, 24, 131, 127, 1), (5, 136, 13, 5, 8)])
+def test_int8_planes(shape, layout, dtype):
+    """The next convolution's activations: at most one step off where 32 bits and 64 bits round apart, and none
+    elsewhere."""
+    from paper_2407_02913_amd import adapt
+
+    for activation in ("relu", "silu"):
+        x, weight, bias, _ = make(shape, dtype, layout, seed=5)
+        scale = 4.0 / 127
+        q = adapt.group_norm_i8(x, shape[4], weight, bias, 1e-5, activation, y_scale=scale)
+        assert q.dtype == torch.int8 and q.is_contiguous()
+        y = reference(x, shape[4], weight, bias, 1e-5, activation)[0]
+        steps = y / scale
+        want = torch.round(steps).clamp(-127, 127)
+        off = (q.double() - want).abs()
+        slack = ((1e-5 + 8 * U * spread(x, shape[4], 1e-5)) * max(1.0, float(y.abs().max())) / scale)
+        tie = ((steps - torch.floor(steps)) - 0.5).abs() <= slack + 1e-5
+        assert (off <= 1).all() and (off[~tie] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 6, 3, 5, 3), (3, 46, 7, 9, 2), (2, 64, 56, 56, 32), (1, 512, 7, 7, 32), (1, 130, 9, 67, 2)])
+@pytest.mark.parametrize("dtype,out", [(torch.float32, torch.float32), (torch.float32, torch.bfloat16),
+                                       (torch.float32, torch.float16), (torch.float16, torch.float16),
+                                       (torch.bfloat16, torch.bfloat16)])
+def test_change_of_layout_and_type(shape, dtype, out):
+    from paper_2407_02913_amd import adapt
+
+    for layout in ("nchw", "nhwc"):
+        x, weight, bias, _ = make(shape, dtype, layout, seed=2)
+        ref = reference(x, shape[4], weight, bias, 1e-5, "silu")[0]
+        for last in (False, True):
+            y, stats = adapt.group_norm_forward(x, shape[4], weight, bias, 1e-5, "silu", dtype=out, channels_last=last)
+            assert y.dtype == out
+            assert y.is_contiguous(memory_format=torch.channels_last if last else torch.contiguous_format)
+            assert ((y.double() - ref).abs() <= bound(ref, x, shape[4], 1e-5, out)).all()
+            same = adapt.group_norm_forward(x, shape[4], weight, bias, 1e-5, "silu")[1]
+            assert torch.allclose(stats, same, rtol=1e-4, atol=1e-4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_strides(layout, dtype):
+    """Channels out of a wider tensor, every second image, an odd first element: the same bits as a copy's."""
+    from paper_2407_02913_amd import adapt
+
+    for shape in [(6, 48, 7, 9, 4), (4, 24, 61, 67, 2)]:
+        n, c, h, w, groups = shape
+        x, weight, bias, dy = make((n, c, h, w, groups), dtype, layout, seed=3)
+        order = torch.channels_last if layout == "nhwc" else torch.contiguous_format
+        wide = torch.full((2 * n, c + 9, h, w), 7.0, dtype=dtype, device="cuda").contiguous(memory_format=order)
+        wide_dy = wide.clone(memory_format=torch.preserve_format)
+        xs, ds = wide[::2, 3:3 + c], wide_dy[::2, 3:3 + c]
+        xs.copy_(x)
+        ds.copy_(dy)
+        a, sa = adapt.group_norm_forward(x, groups, weight, bias, activation="silu")
+        b, sb = adapt.group_norm_forward(xs, groups, weight, bias, activation="silu")
+        tol = 1e-5 + STEP[dtype] * 4
+        assert torch.allclose(a.float(), b.float(), rtol=tol, atol=tol) and torch.allclose(sa, sb, rtol=1e-5, atol=1e-5)
+        ga = adapt.group_norm_backward(dy, x, sa, groups, weight, bias, activation="silu")
+        gb = adapt.group_norm_backward(ds, xs, sa, groups, weight, bias, activation="silu")
+        for p, q in zip(ga, gb):
+            assert torch.allclose(p.float(), q.float(), rtol=1e-4 + 4 * STEP[dtype], atol=(1e-5 + 2 * STEP[dtype]) * float(p.float().abs().max()))
+        assert (wide[1::2] == 7).all() and (wide[:, :3] == 7).all() and (wide[:, 3 + c:] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("shape", [(4, 32, 14, 14, 8), (2, 16, 130, 127, 2)])
+def test_mean_far_from_zero(layout, shape):
+    """A spread a thousandth of the mean: sums of squares would lose it, squares about the mean do not."""
+    from paper_2407_02913_amd import adapt
+
+    x, weight, bias, _ = make(shape, torch.float32, layout, seed=1)
+    x = x * 0.01 + 100.0
+    y, _ = adapt.group_norm_forward(x, shape[4], weight, bias, 1e-12)
+    ref = reference(x, shape[4], weight, bias, 1e-12, "none")[0]
+    assert ((y.double() - ref).abs() <= bound(ref, x, shape[4], 1e-12, torch.float32)).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("shape", [(2, 24, 5, 7, 4), (1, 24, 130, 127, 4)])
+def test_a_broken_value_stays_in_its_group(layout, value, shape):
+    from paper_2407_02913_amd import adapt
+
+    x, weight, bias, dy = make(shape, torch.float32, layout, seed=4)
+    clean, cstats = adapt.group_norm_forward(x, 4, weight, bias, activation="relu")
+    broken = x.clone(memory_format=torch.preserve_format)
+    broken[0, 7, 3, 3] = value
+    y, stats = adapt.group_norm_forward(broken, 4, weight, bias, activation="relu")
+    bad = torch.zeros_like(y, dtype=torch.bool)
+    bad[0, 6:12] = True
+    assert torch.isnan(y[bad]).all() and torch.equal(y[~bad], clean[~bad])
+    dx, _, _ = adapt.group_norm_backward(dy, broken, stats, 4, weight, bias, activation="relu")
+    cdx, _, _ = adapt.group_norm_backward(dy, x, cstats, 4, weight, bias, activation="relu")
+    assert torch.equal(dx[~bad], cdx[~bad])
+
+
+@pytest.mark.gpu
+def test_one_value_to_a_group_has_no_gradient():
+    from paper_2407_02913_amd import adapt
+
+    x, weight, bias, dy = make((3, 8, 1, 1, 8), torch.float32, "nhwc")
+    _, stats = adapt.group_norm_forward(x, 8, weight, bias)
+    dx, dw, db = adapt.group_norm_backward(dy, x, stats, 8, weight, bias)
+    assert (dx == 0).all() and (dw == 0).all() and torch.allclose(db, dy.sum((0, 2, 3)), atol=1e-6)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 12, 5, 7, 3), (1, 6, 90, 91, 1)])
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_gradient_against_differences(shape, layout):
+    """Directional differences of the 64-bit loss sum(y dy), through autograd's entry."""
+    from paper_2407_02913_amd import adapt
+
+    x, weight, bias, dy = make(shape, torch.float32, layout, seed=6)
+    leaves = [t.requires_grad_(True) for t in (x, weight, bias)]
+    grads = torch.autograd.grad(adapt.group_norm(x, shape[4], weight, bias, 1e-5, "gelu"), leaves, dy)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    loss = lambda *p: float((reference(p[0], shape[4], p[1], p[2], 1e-5, "gelu")[0] * dy.double()).sum())  # noqa: E731
+    at = [t.detach().double() for t in leaves]
+    for i in range(3):
+        v = torch.randn(at[i].shape, generator=g, device="cuda").double()
+        step = [t + (1e-4 * v if k == i else 0) for k, t in enumerate(at)]
+        back = [t - (1e-4 * v if k == i else 0) for k, t in enumerate(at)]
+        difference = (loss(*step) - loss(*back)) / 2e-4
+        slope = float((grads[i].double() * v).sum())
+        # the third derivative's share (1e-8) and the gradient's own rounding, over the terms' magnitudes
+        assert abs(slope - difference) <= 2e-5 * float((grads[i].double().abs() * v.abs()).sum()) + 1e-5
+
+
+@pytest.mark.gpu
+def test_nothing_to_do_and_repeatability():
+    from paper_2407_02913_amd import adapt
+
+    for shape in [(0, 8, 3, 3), (2, 8, 0, 3)]:
+        x = torch.empty(shape, device="cuda")
+        w = torch.ones(8, device="cuda")
+        y, stats = adapt.group_norm_forward(x, 4, w, w)
+        dx, dw, db = adapt.group_norm_backward(y, x, stats, 4, w, w)
+        assert y.shape == x.shape and dx.shape == x.shape and (dw == 0).all() and (db == 0).all()
+    for layout in ("nchw", "nhwc"):
+        for shape in [(7, 184, 31, 45, 8), (1, 24, 131, 127, 1)]:
+            x, w, b, dy = make(shape, torch.bfloat16, layout)
+            first = adapt.group_norm_forward(x, shape[4], w, b, activation="silu")
+            first += adapt.group_norm_backward(dy, x, first[1], shape[4], w, b, activation="silu")
+            for _ in range(3):
+                again = adapt.group_norm_forward(x, shape[4], w, b, activation="silu")
+                again += adapt.group_norm_backward(dy, x, again[1], shape[4], w, b, activation="silu")
+                assert all(torch.equal(p, q) for p, q in zip(first, again))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_streams_and_graphs(layout):
+    """Another stream than the default one, and a captured graph replayed between eager work."""
+    from paper_2407_02913_amd import adapt
+
+    shape = (2, 48, 61, 67, 2)
+    x, w, b, dy = make(shape, torch.bfloat16, layout)
+    torch.cuda.synchronize()
+
+    def step():
+        y, stats = adapt.group_norm_forward(x, 2, w, b, activation="silu")
+        return (y, *adapt.group_norm_backward(dy, x, stats, 2, w, b, activation="silu"))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step()
+    torch.cuda.synchronize()
+    for k in range(4):
+        x.copy_(make(shape, torch.bfloat16, layout, seed=10 + k)[0])
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, out))
+
+
+def _desc(**kw):
+    from paper_2407_02913_amd import binding
+
+    d = dict(N=2, C=8, H=3, W=5, groups=4, x_type=0, y_type=0, x_layout=0, y_layout=0, activation=0, eps=1e-5,
+             y_scale=0.0, x_image_stride=0, x_row_stride=0, y_image_stride=0, y_row_stride=0)
+    d.update(kw)
+    return binding.GroupNormDesc(**d)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"groups": 3}, 1), ({"groups": 0}, 1), ({"C": 0}, 1), ({"N": -1}, 1), ({"H": -2}, 1), ({"x_type": 3}, 1),
+    ({"x_type": 4}, 1), ({"y_type": -1}, 1), ({"x_layout": 2}, 1), ({"activation": 4}, 1), ({"eps": -1.0}, 1),
+    ({"eps": math.nan}, 1), ({"y_type": 3}, 1), ({"y_type": 3, "y_scale": 0.1, "y_layout": 1}, 2),
+    ({"x_type": 1, "y_type": 2}, 2), ({"x_type": 1, "y_type": 0}, 2), ({"C": 4097, "groups": 1}, 2),
+    ({"H": 32768, "W": 32768}, 2), ({"x_row_stride": 14}, 1), ({"x_image_stride": -1}, 1), ({"y_row_stride": 3}, 1),
+    ({"N": 1 << 25}, 2),
+])
+def test_bad_descriptions(kw, code):
+    from paper_2407_02913_amd import binding
+
+    lib = binding.load()
+    d = _desc(**kw)
+    assert lib.sfc_group_norm_sizes(C.addressof(d), None, None) == code
+    assert lib.sfc_group_norm(C.addressof(d), 256, None, None, 256, 256, 256, 1 << 20, None) == code
+
+
+def test_bad_pointers_and_workspaces():
+    """Refused before any launch: no GPU is needed."""
+    from paper_2407_02913_amd import binding
+
+    lib = binding.load()
+    d = _desc(N=1, C=24, H=131, W=127, groups=1)
+    at, f, b = C.addressof(d), C.c_size_t(), C.c_size_t()
+    assert lib.sfc_group_norm_sizes(at, C.byref(f), C.byref(b)) == 0 and f.value > 0 and b.value > 0
+    assert lib.sfc_group_norm_sizes(None, None, None) == 1
+    big = 1 << 30
+    assert lib.sfc_group_norm(at, None, None, None, 256, 256, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 256, None, None, None, 256, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 256, None, None, 256, None, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 258, None, None, 256, 256, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 256, 2, None, 256, 256, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 256, None, None, 256, 256, None, big, None) == 6
+    assert lib.sfc_group_norm(at, 256, None, None, 256, 256, 256, f.value - 1, None) == 6
+    assert lib.sfc_group_norm_backward(at, 256, 256, None, None, 256, 256, 256, 256, 256, b.value - 1, None) == 6
+    assert lib.sfc_group_norm_backward(at, 256, None, None, None, 256, 256, 256, 256, 256, big, None) == 1
+    assert lib.sfc_group_norm_backward(at, 256, 256, None, None, None, 256, 256, 256, 256, big, None) == 1
+    for other in (_desc(y_layout=1), _desc(y_type=2)):  # forward only
+        assert lib.sfc_group_norm_backward(C.addressof(other), 256, 256, None, None, 256, 256, 256, 256, 256, big, None) == 2
+
+
+@pytest.mark.gpu
+def test_bad_tensors():
+    from paper_2407_02913_amd import adapt, binding
+
+    x = torch.randn(2, 8, 4, 4, device="cuda")
+    w = torch.ones(8, device="cuda")
+    with pytest.raises(ValueError):
+        adapt.group_norm(x.cpu(), 4)
+    with pytest.raises(ValueError):
+        adapt.group_norm(x[0], 4)
+    with pytest.raises(ValueError):
+        adapt.group_norm(x.double(), 4)
+    with pytest.raises(ValueError):
+        adapt.group_norm(x, 4, w[:4])
+    with pytest.raises(ValueError):
+        adapt.group_norm(x, 4, w.half())
+    with pytest.raises(ValueError):
+        adapt.group_norm(x, 4, activation="tanh")
+    with pytest.raises(ValueError):
+        adapt.group_norm(x.permute(0, 2, 3, 1).transpose(1, 2), 2)
+    with pytest.raises(binding.SfcError):
+        adapt.group_norm(x, 3)
+    y, stats = adapt.group_norm_forward(x, 4, w, w)
+    with pytest.raises(ValueError):
+        adapt.group_norm_backward(y.half(), x, stats, 4, w, w)
+    with pytest.raises(ValueError):
+        adapt.group_norm_backward(y, x, stats[:1], 4, w, w)
