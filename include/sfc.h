@@ -345,6 +345,76 @@ sfc_status sfc_group_norm_backward(const sfc_group_norm_desc* desc, const void* 
                                    void* dx_dev, float* dweight_dev, float* dbias_dev, void* workspace_dev,
                                    size_t workspace_bytes, void* stream);
 
+/* Low-rank adapters of many requests, beside a projection that all requests share:
+ *
+ *   y[t] = base[t] + scale[l] up_l (down_l x[t]),  l = ids[t]
+ *
+ * x [tokens][inputs]; base, y [tokens][outputs], base the shared projection's output (NULL: zeros); down
+ * [adapters][rank][inputs] and up [adapters][outputs][rank], dense; one type.  ids, int32 [tokens]: any order, best
+ * tokens of one adapter side by side; an id outside [0, adapters) is no adapter, y = base.  scale, float32
+ * [adapters], or NULL for ones.  Limits: rank <= 128, adapters <= 2^16, inputs and outputs <= 2^20, tokens <= 2^26. */
+typedef struct {
+  int64_t tokens; /* may be 0 */
+  int32_t inputs, outputs, rank, adapters;
+  int32_t type; /* sfc_type: float32, float16 or bfloat16 */
+  /* from row to row, 0: dense.  y_stride: of y, backward of dy; base_stride: of base, backward of dx_base;
+   * dx_stride: backward only. */
+  int64_t x_stride, base_stride, y_stride, dx_stride;
+} sfc_lowrank_desc;
+
+/* Bytes of workspace (device, 16-byte aligned) of the two calls; either pointer may be NULL. */
+sfc_status sfc_lowrank_sizes(const sfc_lowrank_desc* desc, size_t* forward_bytes, size_t* backward_bytes);
+/* y_dev may be base_dev (with its stride). */
+sfc_status sfc_lowrank_add(const sfc_lowrank_desc* desc, const void* x_dev, const int32_t* ids_dev,
+                           const void* down_dev, const void* up_dev, const float* scale_dev,
+                           const void* base_dev, void* y_dev, void* workspace_dev, size_t workspace_bytes,
+                           void* stream);
+/* From y's gradient dy: dx = dx_base + scale down_l^T up_l^T dy (dx_base, the shared projection's part, may be NULL or
+ * dx_dev itself with its stride), and the factors' gradients, as down and up lie, over all tokens of an adapter (zeros
+ * where it has none). */
+sfc_status sfc_lowrank_backward(const sfc_lowrank_desc* desc, const void* x_dev, const void* dy_dev,
+                                const int32_t* ids_dev, const void* down_dev, const void* up_dev,
+                                const float* scale_dev, const void* dx_base_dev, void* dx_dev,
+                                void* d_down_dev, void* d_up_dev, void* workspace_dev,
+                                size_t workspace_bytes, void* stream);
+
+/* Distillation from a teacher's top logits.  A row holds the student's logits s over all classes and, of the
+ * teacher, `top` places with a value each.  With q = softmax(s / temperature):
+ *
+ *   p = softmax(values / temperature) over the row's places
+ *   loss = temperature^2 sum p (log p - log q)
+ *
+ * or, with `tail`, the values are the teacher's log-probabilities at that temperature, p = exp(values), and the
+ * rest 1 - sum p is one more outcome, against the student's sum of q outside the places.  A place outside
+ * [0, classes) holds nothing (padding); places given twice add up in the loss and the gradient.  A row without any
+ * has loss and gradient 0.
+ * row_scale_dev, float32 [rows] or NULL for ones: the gradient of row r is row_scale[r] times that of its loss (the
+ * loss itself is not scaled); a row of scale 0 is masked: it is not read, its loss and gradient are 0.
+ * Limits: classes <= 2^18, 1 <= top <= 1024. */
+typedef struct {
+  int64_t rows; /* may be 0 */
+  int32_t classes, top;
+  int32_t type;        /* sfc_type of logits and gradient: float32, float16 or bfloat16 */
+  int32_t index_wide;  /* places: 0 int32, 1 int64 */
+  int32_t tail;        /* 0, 1 */
+  float temperature;   /* > 0 */
+  int64_t logits_stride, grad_stride, values_stride, index_stride; /* from row to row; 0: dense */
+} sfc_distill_desc;
+
+/* loss_dev: float32 [rows], unscaled.  stats_dev: float32 [rows][4], what sfc_distill_grad takes, or NULL. */
+sfc_status sfc_distill_loss(const sfc_distill_desc* desc, const void* logits_dev, const float* values_dev,
+                            const void* index_dev, const float* row_scale_dev, float* loss_dev,
+                            float* stats_dev, void* stream);
+/* grad_dev [rows][classes] from the loss call's stats; rows masked there or here are 0.  May be logits_dev
+ * (with its stride). */
+sfc_status sfc_distill_grad(const sfc_distill_desc* desc, const void* logits_dev, const float* values_dev,
+                            const void* index_dev, const float* row_scale_dev, const float* stats_dev,
+                            void* grad_dev, void* stream);
+/* Both, with the logits read once: what a training step calls whose loss is a weighted sum over rows. */
+sfc_status sfc_distill_loss_grad(const sfc_distill_desc* desc, const void* logits_dev, const float* values_dev,
+                                 const void* index_dev, const float* row_scale_dev, float* loss_dev,
+                                 void* grad_dev, void* stream);
+
 /* Measurement aid: a plain streaming copy of `bytes` (a multiple of 16, both
  * pointers 16-byte aligned) from src_dev to dst_dev on `stream`.  It reads and
  * writes every byte exactly once, so hardware byte counters and achieved-bandwidth

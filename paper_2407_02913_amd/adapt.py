@@ -7,6 +7,9 @@ shapes, types and devices here (``ValueError``).
 
 * ``group_norm``: group norm with an activation, channels last or planes; ``group_norm_i8`` hands on the
   next convolution's int8 activations.
+* ``adapters``: low-rank adapters of many requests, added to a projection that all of them share.
+* ``distill``: the loss of a student's logits against a teacher's top ones; ``distill_loss_and_grad`` gives
+  the gradient in the same pass over the logits.
 """
 from __future__ import annotations
 
@@ -181,3 +184,192 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none"):
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
         return _GroupNorm.apply(x, weight, bias, groups, eps, activation)
     return group_norm_forward(x, groups, weight, bias, eps, activation)[0]
+
+
+# ---- low-rank adapters ----
+
+class _Lowrank:
+    """A description with its workspace sizes."""
+
+    def __init__(self, *fields):
+        self.desc = binding.LowrankDesc(*fields)
+        self.at = C.addressof(self.desc)
+        forward, backward = C.c_size_t(), C.c_size_t()
+        binding._check(binding.load().sfc_lowrank_sizes(self.at, C.byref(forward), C.byref(backward)),
+                       "sfc_lowrank_sizes")
+        self.forward_bytes, self.backward_bytes = forward.value, backward.value
+
+
+_lowrank = lru_cache(maxsize=1024)(_Lowrank)
+
+
+def _row_stride(t, what):
+    _require(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: a row's values lie side by side, not strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _check_adapters(x, ids, down, up, scale, outputs, wide):
+    """`outputs`, `wide`: (name, tensor or None) with as many columns as `up` has outputs, `down` inputs."""
+    _require(x.is_cuda and x.dim() == 2, f"x: [tokens, inputs] on the GPU, not {tuple(x.shape)} on {x.device}")
+    _require(x.dtype in _TYPE and x.dtype != torch.int8, f"x: float32, float16 or bfloat16, not {x.dtype}")
+    tokens, inputs = x.shape
+    _require(down.dim() == 3 and down.shape[2] == inputs and down.dtype == x.dtype and down.is_contiguous()
+             and down.device == x.device, f"down: {x.dtype} [adapters, rank, {inputs}] on {x.device}, contiguous")
+    adapters, rank, _ = down.shape
+    _require(up.dim() == 3 and up.shape[0] == adapters and up.shape[2] == rank and up.dtype == x.dtype
+             and up.is_contiguous() and up.device == x.device,
+             f"up: {x.dtype} [{adapters}, outputs, {rank}] on {x.device}, contiguous")
+    _require(ids.shape == (tokens,) and ids.dtype == torch.int32 and ids.is_contiguous() and ids.device == x.device,
+             f"ids: int32 [{tokens}] on {x.device}, contiguous")
+    if scale is not None:
+        _require(scale.shape == (adapters,) and scale.dtype == torch.float32 and scale.is_contiguous()
+                 and scale.device == x.device, f"scale: float32 [{adapters}] on {x.device}, contiguous")
+    for columns, tensors in ((up.shape[1], outputs), (inputs, wide)):
+        for name, t in tensors:
+            _require(t is None or (t.shape == (tokens, columns) and t.dtype == x.dtype and t.device == x.device),
+                     f"{name}: {x.dtype} [{tokens}, {columns}] on {x.device}")
+    return tokens, inputs, up.shape[1], rank, adapters, _TYPE[x.dtype]
+
+
+def add_adapters(base, x, ids, down, up, scale=None, out=None):
+    """y[t] = base[t] + scale[l] up[l] (down[l] x[t]), l = ids[t]: the low-rank adapters of many requests, beside a
+    projection that all of them share.
+
+    x [tokens, inputs]; base [tokens, outputs], the shared projection's output, or None; down [adapters, rank, inputs] and
+    up [adapters, outputs, rank]; one type, float32, float16 or bfloat16.  ids, int32 [tokens]: any order; an id
+    outside the adapters is none, y = base.  scale, float32 [adapters], or None.  `out` may be base."""
+    fields = _check_adapters(x, ids, down, up, scale, (("base", base), ("out", out)), ())
+    y = torch.empty((fields[0], fields[2]), dtype=x.dtype, device=x.device) if out is None else out
+    plan = _lowrank(*fields, _row_stride(x, "x"), 0 if base is None else _row_stride(base, "base"), _row_stride(y, "out"), 0)
+    space = _bytes(plan.forward_bytes, x.device)
+    _call(x.device, "sfc_lowrank_add", plan.at, x.data_ptr(), ids.data_ptr(), down.data_ptr(), up.data_ptr(), _ptr(scale),
+          _ptr(base), y.data_ptr(), _ptr(space), plan.forward_bytes)
+    return y
+
+
+def add_adapters_backward(dy, x, ids, down, up, scale=None, dx_base=None):
+    """(dx, d_down, d_up) from y's gradient dy: dx = dx_base + scale[l] (up[l] down[l])^T dy, where dx_base is the shared
+    projection's part or None; the factors' gradients, in their type, are sums over each adapter's tokens."""
+    fields = _check_adapters(x, ids, down, up, scale, (("dy", dy),), (("dx_base", dx_base),))
+    dx = torch.empty((fields[0], fields[1]), dtype=x.dtype, device=x.device)
+    d_down, d_up = torch.empty_like(down), torch.empty_like(up)
+    plan = _lowrank(*fields, _row_stride(x, "x"), 0 if dx_base is None else _row_stride(dx_base, "dx_base"),
+                    _row_stride(dy, "dy"), 0)
+    space = _bytes(plan.backward_bytes, x.device)
+    _call(x.device, "sfc_lowrank_backward", plan.at, x.data_ptr(), dy.data_ptr(), ids.data_ptr(), down.data_ptr(),
+          up.data_ptr(), _ptr(scale), _ptr(dx_base), dx.data_ptr(), d_down.data_ptr(), d_up.data_ptr(), _ptr(space),
+          plan.backward_bytes)
+    return dx, d_down, d_up
+
+
+class _Adapters(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, base, x, ids, down, up, scale):
+        ctx.save_for_backward(x, ids, down, up, scale)
+        ctx.with_base = base is not None
+        return add_adapters(base, x, ids, down, up, scale)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, ids, down, up, scale = ctx.saved_tensors
+        dy = dy.contiguous()
+        dx, d_down, d_up = add_adapters_backward(dy, x, ids, down, up, scale)
+        return dy if ctx.with_base else None, dx, None, d_down, d_up, None
+
+
+def adapters(base, x, ids, down, up, scale=None):
+    """y of add_adapters; differentiable in base, x, down and up."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (base, x, down, up)):
+        return _Adapters.apply(base, x, ids, down, up, scale)
+    return add_adapters(base, x, ids, down, up, scale)
+
+
+# ---- distillation from a teacher's top logits ----
+
+@lru_cache(maxsize=1024)
+def _distill(rows, classes, top, dtype, wide, tail, temperature, logits_stride, grad_stride, values_stride, index_stride):
+    return binding.DistillDesc(rows, classes, top, _TYPE[dtype], int(wide), int(tail), temperature,
+                               logits_stride, grad_stride, values_stride, index_stride)
+
+
+def _check_distill(logits, values, index, row_scale, temperature, tail, grad=None):
+    _require(logits.is_cuda and logits.dim() == 2 and logits.shape[1] > 0,
+             f"logits: [rows, classes] on the GPU, not {tuple(logits.shape)} on {logits.device}")
+    _require(logits.dtype in _TYPE and logits.dtype != torch.int8,
+             f"logits: float32, float16 or bfloat16, not {logits.dtype}")
+    rows, classes = logits.shape
+    _require(values.dim() == 2 and values.shape[0] == rows and values.dtype == torch.float32
+             and values.device == logits.device, f"values: float32 [{rows}, top] on {logits.device}")
+    _require(index.shape == values.shape and index.dtype in (torch.int32, torch.int64) and index.device == logits.device,
+             f"index: int32 or int64 {tuple(values.shape)} on {logits.device}")
+    if row_scale is not None:
+        _require(row_scale.shape == (rows,) and row_scale.dtype == torch.float32 and row_scale.is_contiguous()
+                 and row_scale.device == logits.device, f"row_scale: float32 [{rows}] on {logits.device}, contiguous")
+    desc = _distill(rows, classes, values.shape[1], logits.dtype, index.dtype == torch.int64, tail, temperature,
+                    _row_stride(logits, "logits"), 0 if grad is None else _row_stride(grad, "grad"),
+                    _row_stride(values, "values"), _row_stride(index, "index"))
+    return C.addressof(desc)
+
+
+def distill_loss(logits, values, index, row_scale=None, temperature=1.0, tail=False):
+    """(loss, stats) of each row: the divergence of q = softmax(logits / temperature) from the teacher's p, times
+    temperature^2, float32 [rows]; stats, float32 [rows, 4], for distill_grad.
+
+    values, float32 [rows, top], and index, int32 or int64, are the teacher's top logits and their places; p is
+    their softmax at the temperature.  tail: the values are log-probabilities at the temperature instead, and what
+    they leave is one more outcome, against the student's mass outside the places.  A place outside the classes
+    is padding.  row_scale, float32 [rows]: rows of 0 are masked (loss 0, not read)."""
+    at = _check_distill(logits, values, index, row_scale, temperature, tail)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    stats = torch.empty((logits.shape[0], 4), dtype=torch.float32, device=logits.device)
+    _call(logits.device, "sfc_distill_loss", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
+          loss.data_ptr(), stats.data_ptr())
+    return loss, stats
+
+
+def distill_grad(logits, values, index, stats, row_scale=None, temperature=1.0, tail=False, out=None):
+    """The gradient of sum(row_scale loss) in the logits, in their type, from distill_loss's stats.  `out` may be
+    the logits themselves."""
+    grad = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+    _require(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device,
+             f"out: as the logits, {tuple(logits.shape)} {logits.dtype}")
+    _require(stats.shape == (logits.shape[0], 4) and stats.dtype == torch.float32 and stats.is_contiguous()
+             and stats.device == logits.device, f"stats: float32 [{logits.shape[0]}, 4], as distill_loss gave them")
+    at = _check_distill(logits, values, index, row_scale, temperature, tail, grad)
+    _call(logits.device, "sfc_distill_grad", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
+          stats.data_ptr(), grad.data_ptr())
+    return grad
+
+
+def distill_loss_and_grad(logits, values, index, row_scale=None, temperature=1.0, tail=False, out=None):
+    """(loss, gradient) as of distill_loss and distill_grad, the logits read once: for a training step whose loss
+    is sum(row_scale loss)."""
+    grad = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
+    _require(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device,
+             f"out: as the logits, {tuple(logits.shape)} {logits.dtype}")
+    at = _check_distill(logits, values, index, row_scale, temperature, tail, grad)
+    loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
+    _call(logits.device, "sfc_distill_loss_grad", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(),
+          _ptr(row_scale), loss.data_ptr(), grad.data_ptr())
+    return loss, grad
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, values, index, mask, temperature, tail):
+        loss, stats = distill_loss(logits, values, index, mask, temperature, tail)
+        ctx.save_for_backward(logits, values, index, mask, stats)
+        ctx.how = temperature, tail
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        logits, values, index, mask, stats = ctx.saved_tensors
+        scale = dloss.contiguous() if mask is None else torch.where(mask != 0, dloss, 0.0)
+        return (distill_grad(logits, values, index, stats, scale, *ctx.how),) + (None,) * 5
+
+
+def distill(logits, values, index, mask=None, temperature=1.0, tail=False):
+    """loss of distill_loss, float32 [rows]; differentiable in the logits.  mask, float32 [rows]: rows of 0 have
+    loss and gradient 0."""
+    return _Distill.apply(logits, values, index, mask, temperature, tail)

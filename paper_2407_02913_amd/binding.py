@@ -43,6 +43,8 @@ EXPORTS = (
     "sfc_calibrate_act_scales", "sfc_calibrate_filter_scales", "sfc_transform_filter",
     "sfc_conv2d_nchw", "sfc_conv2d_nchw_static", "sfc_conv2d_stages", "sfc_tap_info", "sfc_stream_copy", "sfc_status_string",
     "sfc_group_norm_sizes", "sfc_group_norm", "sfc_group_norm_backward",
+    "sfc_lowrank_sizes", "sfc_lowrank_add", "sfc_lowrank_backward",
+    "sfc_distill_loss", "sfc_distill_grad", "sfc_distill_loss_grad",
 )
 
 
@@ -62,6 +64,19 @@ class GroupNormDesc(C.Structure):
                                           "activation")]
                 + [(n, C.c_float) for n in ("eps", "y_scale")]
                 + [(n, C.c_int64) for n in ("x_image_stride", "x_row_stride", "y_image_stride", "y_row_stride")])
+
+
+class LowrankDesc(C.Structure):
+    _fields_ = ([("tokens", C.c_int64)]
+                + [(n, C.c_int32) for n in ("inputs", "outputs", "rank", "adapters", "type")]
+                + [(n, C.c_int64) for n in ("x_stride", "base_stride", "y_stride", "dx_stride")])
+
+
+class DistillDesc(C.Structure):
+    _fields_ = ([("rows", C.c_int64)]
+                + [(n, C.c_int32) for n in ("classes", "top", "type", "index_wide", "tail")]
+                + [("temperature", C.c_float)]
+                + [(n, C.c_int64) for n in ("logits_stride", "grad_stride", "values_stride", "index_stride")])
 
 
 class SfcError(RuntimeError):
@@ -124,6 +139,18 @@ def load(force: bool = False):
     lib.sfc_group_norm.restype = i32
     lib.sfc_group_norm_backward.argtypes = [vp] * 10 + [C.c_size_t, vp]
     lib.sfc_group_norm_backward.restype = i32
+    lib.sfc_lowrank_sizes.argtypes = [vp, size_p, size_p]
+    lib.sfc_lowrank_sizes.restype = i32
+    lib.sfc_lowrank_add.argtypes = [vp] * 9 + [C.c_size_t, vp]
+    lib.sfc_lowrank_add.restype = i32
+    lib.sfc_lowrank_backward.argtypes = [vp] * 12 + [C.c_size_t, vp]
+    lib.sfc_lowrank_backward.restype = i32
+    lib.sfc_distill_loss.argtypes = [vp] * 8
+    lib.sfc_distill_loss.restype = i32
+    lib.sfc_distill_grad.argtypes = [vp] * 8
+    lib.sfc_distill_grad.restype = i32
+    lib.sfc_distill_loss_grad.argtypes = [vp] * 8
+    lib.sfc_distill_loss_grad.restype = i32
     lib.sfc_status_string.argtypes = [i32]
     lib.sfc_status_string.restype = C.c_char_p
     _lib = lib

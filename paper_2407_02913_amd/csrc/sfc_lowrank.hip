@@ -1,0 +1,625 @@
+// Low-rank adapters of many requests, added to a projection that all requests share.
+//
+//   h[t] = down_l x[t],  y[t] = base[t] + scale_l up_l h[t],  l = ids[t]  (none outside [0, adapters): y = base)
+//
+// Two kernels: `shrink` (x and the adapters' down factors are read, h, a row of `rank` floats a token, is left in the
+// workspace) and `expand`.  The work is reading x, base and writing y: 2 rank operations a value, some tens where HBM
+// allows some hundreds.
+//
+// Up to kFew tokens (single tokens, each perhaps with an adapter of its own) the adapters' factors are most of the
+// bytes and every token reads its own: rows of them go straight to vector arithmetic, a wave to a row of `down`, a lane
+// to a row of `up`, spread over as many workgroups as there are rows.  Above, tokens come in tiles for the matrix
+// cores.  A tile's tokens mostly share an adapter; where they do not, each adapter of the tile takes its turn over all
+// of them and keeps its own tokens' results.
+//
+// Gradients: with G = dy up_l (a shrink with the transposed up factors), dx = dx_base + scale_l G down_l (an expand with
+// the transposed down factors), d down_l = scale_l sum G[t] x[t]^T and d up_l = scale_l sum dy[t] h[t]^T (`outer`).  The
+// banks are transposed into the workspace first; they are small beside x and dy.
+#include "sfc_lowrank.hpp"
+
+namespace sfc {
+namespace {
+
+constexpr int kFew = 256;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// acc += a b^T of 16x16 results over a vector's elements in each of the four lane groups: lane l holds the elements
+// V (l / 16) .. + V - 1 of row l % 16 of both operands.  Which four numbers a matrix instruction pairs does not
+// matter as long as both operands agree, so float32 takes an element at a time.  Result: column l % 16 (of b's rows),
+// rows 4 (l / 16) + 0..3 (of a's).
+template <typename T>
+__device__ __forceinline__ v4f mma(const raw4& a, const raw4& b, v4f acc) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), acc, 0, 0, 0);
+    return acc;
+  } else if constexpr (__is_same(T, bf16)) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0,
+                                                   0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0,
+                                                  0);
+  }
+}
+
+// Floats of a token's row in the workspace.
+__host__ __device__ inline int row_of(int rank) { return (rank + 7) / 8 * 8; }
+
+// ---- few tokens ----
+
+template <typename T>
+__global__ __launch_bounds__(256) void shrink_few(const T* x, int64_t x_stride, const int32_t* ids, const T* down, float* h,
+                                                  int tokens, int inputs, int rank, int adapters) {
+  constexpr int V = kVec<T>;
+  const int t = blockIdx.x, l = ids[t], r = blockIdx.y * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (l < 0 || l >= adapters || r >= rank) return;
+  const T* row = x + t * x_stride;
+  const int64_t at = ((int64_t)l * rank + r) * inputs;
+  const int64_t room = (int64_t)adapters * rank * inputs - at, room_x = (tokens - 1 - t) * x_stride + inputs;
+  const T* w = down + at;
+  float s = 0.0f;
+  for (int k0 = lane * V; k0 < inputs; k0 += 4 * 64 * V) {
+    raw4 a[4], b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int k = k0 + u * 64 * V;
+      a[u] = b[u] = raw4{0u, 0u, 0u, 0u};
+      if (k < inputs) a[u] = load_cut(row + k, inputs - k, room_x - k), b[u] = load_cut(w + k, inputs - k, room - k);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s = fmaf(element<T>(a[u], j), element<T>(b[u], j), s);
+  }
+  s = wave_sum(s);
+  if (lane == 0) h[(int64_t)t * row_of(rank) + r] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void expand_few(const float* h, const int32_t* ids, const T* up, const float* scale,
+                                                  const T* base, int64_t base_stride, T* y, int64_t y_stride,
+                                                  int outputs, int rank, int adapters) {
+  constexpr int V = kVec<T>;
+  const int t = blockIdx.x, l = ids[t], m = blockIdx.y * 256 + threadIdx.x;
+  if (m >= outputs) return;
+  float v = base ? (float)base[t * base_stride + m] : 0.0f;
+  if (l >= 0 && l < adapters) {
+    const float* ht = h + (int64_t)t * row_of(rank);
+    const int64_t at = ((int64_t)l * outputs + m) * rank, room = (int64_t)adapters * outputs * rank - at;
+    const T* w = up + at;
+    float s = 0.0f;
+    for (int r = 0; r < rank; r += V) {
+      const raw4 a = load_cut(w + r, rank - r, room - r);
+#pragma unroll
+      for (int j = 0; j < V; ++j) s = fmaf(element<T>(a, j), r + j < rank ? ht[r + j] : 0.0f, s);
+    }
+    v = fmaf(scale ? scale[l] : 1.0f, s, v);
+  }
+  y[t * y_stride + m] = (T)v;
+}
+
+// ---- tiles of tokens ----
+
+// One of the products of a shrink launch.
+struct Shrink {
+  const void* x;
+  const void* bank;  // [adapters][rank][inputs]
+  float* h;          // [tokens][row_of(rank)]
+  int64_t stride;
+  int inputs;
+};
+
+constexpr int kTokens = 32;  // of a shrink's tile
+
+// h of 32 tokens: waves share the inputs in turns of 128 bytes a row, and add up in LDS.  RT: sixteens of the rank.
+template <typename T, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, const int32_t* ids, int2* range,
+                                                          int tokens, int rank, int adapters) {
+  constexpr int V = kVec<T>, STEP = 4 * V, CHUNK = 2 * STEP;
+  __shared__ v4f sums[WAVES][RT][2][64];
+  const Shrink p = blockIdx.y ? p1 : p0;
+  const int t0 = blockIdx.x * kTokens, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = lane & 15, group = lane >> 4;
+  const T* x = static_cast<const T*>(p.x);
+  const int64_t end_x = (tokens - 1) * p.stride + p.inputs, end_w = (int64_t)adapters * rank * p.inputs;
+  int64_t at_x[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) at_x[i] = min(t0 + 16 * i + row, tokens - 1) * p.stride + group * V;
+  const int mine = t0 + (lane & 31) < tokens ? ids[t0 + (lane & 31)] : -1;
+  uint64_t left = __ballot(lane < kTokens && mine >= 0 && mine < adapters);
+  while (left) {  // (the same in every wave of the workgroup)
+    const int l = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+    const uint64_t sel = __ballot(lane < kTokens && mine == l);
+    left &= ~sel;
+    if (range && blockIdx.y == 0 && threadIdx.x == 0) {
+      atomicMin(&range[l].x, t0 + (int)__builtin_ctzll(sel));
+      atomicMax(&range[l].y, t0 + 64 - (int)__builtin_clzll(sel));
+    }
+    const T* w = static_cast<const T*>(p.bank);
+    int64_t at_w[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) at_w[r] = ((int64_t)l * rank + min(16 * r + row, rank - 1)) * p.inputs + group * V;
+    v4f acc[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    const int whole = p.inputs / CHUNK * CHUNK;
+    for (int k = wave * CHUNK; k < whole; k += WAVES * CHUNK) {
+      raw4 a[2][2], b[2][RT];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) a[u][i] = load16(x + at_x[i] + k + u * STEP);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) b[u][r] = load16(w + at_w[r] + k + u * STEP);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[r][i] = mma<T>(b[u][r], a[u][i], acc[r][i]);
+    }
+    if (wave == (whole / CHUNK) % WAVES) {  // what is left of the inputs, cut on both sides
+      for (int k = whole; k < p.inputs; k += STEP) {
+        const int valid = p.inputs - k - group * V;
+        raw4 a[2], b[RT];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          a[i] = valid > 0 ? load_cut(x + at_x[i] + k, valid, end_x - at_x[i] - k) : raw4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+          b[r] = valid > 0 ? load_cut(w + at_w[r] + k, valid, end_w - at_w[r] - k) : raw4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) acc[r][i] = mma<T>(b[r], a[i], acc[r][i]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) sums[wave][r][i][lane] = acc[r][i];
+    __syncthreads();
+    for (int s = threadIdx.x; s < RT * 2 * 64; s += WAVES * 64) {
+      const int r = s >> 7, i = s >> 6 & 1, ln = s & 63, t = 16 * i + (ln & 15), first = 16 * r + 4 * (ln >> 4);
+      v4f v = sums[0][r][i][ln];
+#pragma unroll
+      for (int q = 1; q < WAVES; ++q) v += sums[q][r][i][ln];
+      if ((sel >> t & 1) && first < rank)
+        *reinterpret_cast<v4f*>(p.h + (int64_t)(t0 + t) * row_of(rank) + first) = v;
+    }
+    __syncthreads();
+  }
+}
+
+// Ranks [r0, r0 + V) of a token's h, zeros past the rank.
+template <int V>
+__device__ __forceinline__ void load_h(const float* h, int r0, int rank, bool live, float (&v)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; j += 4) {
+    const bool there = live && r0 + j < rank;
+    const v4f q = there ? *reinterpret_cast<const v4f*>(h + r0 + j) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[j + e] = r0 + j + e < rank ? q[e] : 0.0f;
+  }
+}
+
+// acc += a h of one step: a is a vector of the bank's row, h its floats.  bfloat16: h as the sum of two numbers, which
+// keeps 16 of its 24 bits at two instructions; float16: in float32, since h may leave its range.
+template <typename T>
+__device__ __forceinline__ v4f mma_h(const raw4& a, const float (&h)[kVec<T>], v4f acc) {
+  if constexpr (__is_same(T, bf16)) {
+    bf16x8 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      hi[j] = (bf16)h[j];
+      const float rest = h[j] - (float)hi[j];
+      lo[j] = (bf16)(rest == rest ? rest : 0.0f);  // (an infinity leaves no rest)
+    }
+    const bf16x8 w = __builtin_bit_cast(bf16x8, a);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec<T>; ++j)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T>(a, j), h[j], acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+struct Expand {
+  const float* h;
+  const void* bank;  // [adapters][outputs][rank]
+  const void* base;
+  void* y;
+  int64_t base_stride, y_stride;
+  int outputs;
+};
+
+// y of 64 outputs a wave over a run of tokens, sixteen at a time; the bank's rows stay in registers while the adapter
+// stays.  STEPS: of 4 V ranks.
+template <typename T, int STEPS>
+__global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids, const float* scale, int tokens, int rank,
+                                                   int adapters, int run) {
+  constexpr int V = kVec<T>, PARTS = 16 / V;  // 16-byte pieces of a lane's outputs
+  const int lane = threadIdx.x & 63, row = lane & 15, group = lane >> 4;
+  const int m0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 64;
+  if (m0 >= p.outputs) return;
+  const T* bank = static_cast<const T*>(p.bank);
+  const T* base = static_cast<const T*>(p.base);
+  T* y = static_cast<T*>(p.y);
+  const int64_t end_w = (int64_t)adapters * p.outputs * rank;
+  const int64_t end_base = (tokens - 1) * p.base_stride + p.outputs;
+  // Tile a's row i is output m0 + place(a, i): a lane's four results of tiles that belong together are then
+  // neighbours, V of them a piece, and four lane groups' pieces 64 bytes of a token's row.
+  auto place = [](int a, int i) { return (a * 4 / V) * 4 * V + (i >> 2) * V + (a * 4) % V + (i & 3); };
+  raw4 w[4][STEPS];
+  int loaded = -1;
+  const int first = blockIdx.x * run, last = min(tokens, first + run);
+  for (int t0 = first; t0 < last; t0 += 16) {
+    const int t = t0 + row;
+    const bool live = t < last;
+    const int mine = live ? ids[t] : -1;
+    raw4 old[PARTS];
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) {
+      const int m = m0 + q * 4 * V + group * V;
+      old[q] = raw4{0u, 0u, 0u, 0u};
+      if (base && live && m < p.outputs) {
+        const int64_t at = t * p.base_stride + m;
+        old[q] = load_cut(base + at, p.outputs - m, end_base - at);
+      }
+    }
+    v4f acc[4];
+#pragma unroll
+    for (int a = 0; a < 4; ++a) acc[a] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    uint64_t left = __ballot(lane < 16 && mine >= 0 && mine < adapters);
+    while (left) {
+      const int l = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
+      left &= ~__ballot(lane < 16 && mine == l);
+      if (l != loaded) {
+        loaded = l;
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+#pragma unroll
+          for (int s = 0; s < STEPS; ++s) {
+            const int m = m0 + place(a, row), r = (s * 4 + group) * V;
+            const int64_t at = ((int64_t)l * p.outputs + m) * rank + r;
+            w[a][s] = m < p.outputs && r < rank ? load_cut(bank + at, rank - r, end_w - at) : raw4{0u, 0u, 0u, 0u};
+          }
+      }
+      v4f own[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a) own[a] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        float h[V];
+        load_h<V>(p.h + (int64_t)t * row_of(rank), (s * 4 + group) * V, rank, mine == l, h);
+#pragma unroll
+        for (int a = 0; a < 4; ++a) own[a] = mma_h<T>(w[a][s], h, own[a]);
+      }
+      // (chosen, not multiplied by zero: an adapter that holds infinities is no matter of the other tokens)
+      if (mine == l) {
+#pragma unroll
+        for (int a = 0; a < 4; ++a) acc[a] = own[a];
+      }
+    }
+    const float f = mine < 0 || mine >= adapters ? 0.0f : scale ? scale[mine] : 1.0f;
+#pragma unroll
+    for (int q = 0; q < PARTS; ++q) {
+      const int m = m0 + q * 4 * V + group * V;
+      if (live && m < p.outputs) {
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = fmaf(f, acc[q * V / 4 + j / 4][j % 4], element<T>(old[q], j));
+        store_vec<T, V>(y + t * p.y_stride + m, v, p.outputs - m);
+      }
+    }
+  }
+}
+
+// ---- gradients of the factors ----
+
+// [batch][rows][cols] -> [batch][cols][rows], tiles of 64x64; the first workgroups clear the adapters' ranges too.
+template <typename T>
+__global__ __launch_bounds__(256) void transpose_banks(const T* down, T* down_t, const T* up, T* up_t, int2* range,
+                                                       int adapters, int rank, int inputs, int outputs, int tiles_down,
+                                                       int tiles_up) {
+  __shared__ T tile[64][64 + 4 / sizeof(T)];
+  const int id = blockIdx.x;
+  for (int l = id * 256 + threadIdx.x; l < adapters; l += gridDim.x * 256) range[l] = make_int2(0x7fffffff, 0);
+  const bool first = id < tiles_down * adapters;
+  const int rows = first ? rank : outputs, cols = first ? inputs : rank;
+  const int tiles = first ? tiles_down : tiles_up, at = first ? id : id - tiles_down * adapters;
+  const int l = at / tiles, tl = at - l * tiles, across = (cols + 63) / 64;
+  const int r0 = tl / across * 64, c0 = tl % across * 64;
+  const T* from = (first ? down : up) + (int64_t)l * rows * cols;
+  T* to = (first ? down_t : up_t) + (int64_t)l * rows * cols;
+  const int c = threadIdx.x & 63;
+  for (int r = threadIdx.x >> 6; r < 64; r += 4)
+    if (r0 + r < rows && c0 + c < cols) tile[r][c] = from[(int64_t)(r0 + r) * cols + c0 + c];
+  __syncthreads();
+  for (int r = threadIdx.x >> 6; r < 64; r += 4)
+    if (c0 + r < cols && r0 + c < rows) to[(int64_t)(c0 + r) * rows + r0 + c] = tile[c][r];
+}
+
+struct Outer {
+  const float* g;   // [tokens][row_of(rank)]
+  const void* x;    // [tokens][cols]
+  float* part;      // [splits][adapters][rank][cols]
+  int64_t stride;
+  int cols, blocks;  // columns, and their blocks
+};
+
+// sum over an adapter's tokens of g[t][r] x[t][c], for 64 ranks and 16 V columns: four tokens a matrix instruction in
+// float32, which takes x's rows as they lie (lane l has the V columns V (l % 16) .. of token l / 16, element e of all
+// lanes is one operand), so nothing is transposed and g is not rounded.
+template <typename T, int RT>
+__global__ __launch_bounds__(256) void outer_tile(Outer p0, Outer p1, const int32_t* ids, const int2* range, int tokens,
+                                                  int rank, int adapters, int splits) {
+  constexpr int V = kVec<T>;
+  __shared__ v4f sums[2][RT][V][64];
+  const bool second = (int)blockIdx.x >= p0.blocks * adapters;
+  const Outer p = second ? p1 : p0;
+  const int id = second ? blockIdx.x - p0.blocks * adapters : blockIdx.x;
+  const int l = id / p.blocks, c0 = (id - l * p.blocks) * 16 * V, r0 = blockIdx.z * RT * 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, group = lane >> 4;
+  const int2 rg = range[l];
+  v4f acc[RT][V];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[r][e] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  const int lo = rg.x, count = rg.y > rg.x ? rg.y - rg.x : 0;
+  const int each = (count + splits * 16 - 1) / (splits * 16) * 16;
+  const int first = lo + blockIdx.y * each, last = min(rg.y, first + each);
+  const T* x = static_cast<const T*>(p.x);
+  const int64_t end_x = (tokens - 1) * p.stride + p.cols;
+  const int c = c0 + row * V, h_row = row_of(rank);
+  if (count) {
+    for (int t0 = first + wave * 16; t0 < last; t0 += 64) {
+      raw4 xv[4];
+      float gv[4][RT];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int t = t0 + u * 4 + group;
+        const bool mine = t < last && ids[t] == l;
+        xv[u] = raw4{0u, 0u, 0u, 0u};
+        if (mine && c < p.cols) xv[u] = load_cut(x + t * p.stride + c, p.cols - c, end_x - t * p.stride - c);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          const int at = r0 + r * 16 + row;
+          gv[u][r] = mine && at < rank ? p.g[(int64_t)t * h_row + at] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            acc[r][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(gv[u][r], element<T>(xv[u], e), acc[r][e], 0, 0, 0);
+    }
+  }
+  // four waves' sums, two and two
+#pragma unroll
+  for (int half = 2; half; half >>= 1) {
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[wave - half][r][e][lane] = acc[r][e];
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[r][e] += sums[wave][r][e][lane];
+    }
+    __syncthreads();
+  }
+  if (wave == 0) {
+    float* to = p.part + ((int64_t)blockIdx.y * adapters + l) * rank * p.cols;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int at = r0 + r * 16 + group * 4 + i;
+        if (at < rank) {
+          float v[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = acc[r][e][i];
+          if (c < p.cols) {
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+              const float quad[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+              if (c + e < p.cols) store_vec<float, 4>(to + (int64_t)at * p.cols + c + e, quad, p.cols - c - e);
+            }
+          }
+        }
+      }
+  }
+}
+
+// Adds the splits, scales, rounds: d down as it lies, d up transposed.
+template <typename T>
+__global__ __launch_bounds__(256) void outer_finish(const float* part_down, const float* part_up, const float* scale, T* d_down,
+                                                    T* d_up, int rank, int inputs, int outputs, int adapters, int splits,
+                                                    int blocks_down, int blocks_up) {
+  const bool second = (int)blockIdx.x >= blocks_down * adapters;
+  const int id = second ? blockIdx.x - blocks_down * adapters : blockIdx.x;
+  const int blocks = second ? blocks_up : blocks_down, cols = second ? outputs : inputs;
+  const int l = id / blocks, c = (id - l * blocks) * 256 + threadIdx.x;
+  if (c >= cols) return;
+  const float f = scale ? scale[l] : 1.0f;
+  const int64_t split = (int64_t)adapters * rank * cols;
+  const float* from = (second ? part_up : part_down) + (int64_t)l * rank * cols + c;
+  for (int r = blockIdx.y; r < rank; r += gridDim.y) {
+    float v = 0.0f;
+    for (int s = 0; s < splits; ++s) v += from[s * split + (int64_t)r * cols];
+    if (second) d_up[((int64_t)l * outputs + c) * rank + r] = (T)(v * f);
+    else d_down[((int64_t)l * rank + r) * inputs + c] = (T)(v * f);
+  }
+}
+
+size_t up64(size_t v) { return (v + 63) / 64 * 64; }
+
+template <typename T, int RT, int WAVES>
+void run_shrink_as(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
+  const dim3 grid((unsigned)((a.tokens + kTokens - 1) / kTokens), (unsigned)products);
+  shrink_tile<T, RT, WAVES><<<grid, WAVES * 64, 0, s>>>(p0, p1, a.ids, range, a.tokens, a.rank, a.adapters);
+}
+
+template <typename T>
+hipError_t run_shrink(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
+  if (a.rank <= 16) run_shrink_as<T, 1, 8>(p0, p1, products, a, range, s);
+  else if (a.rank <= 32) run_shrink_as<T, 2, 8>(p0, p1, products, a, range, s);
+  else if (a.rank <= 64) run_shrink_as<T, 4, 4>(p0, p1, products, a, range, s);
+  else run_shrink_as<T, 8, 4>(p0, p1, products, a, range, s);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_expand(const Expand& p, const LowrankArgs& a, hipStream_t s) {
+  // runs of tokens: some 2048 workgroups, a run not under 16 tokens
+  const int across = (p.outputs + 255) / 256;
+  int run = (int)(((int64_t)a.tokens * across + 2047) / 2048);
+  run = (run + 15) / 16 * 16;
+  const dim3 grid((unsigned)((a.tokens + run - 1) / run), (unsigned)across);
+  const int steps = (a.rank + 4 * kVec<T> - 1) / (4 * kVec<T>);
+  if (steps <= 1) expand_tile<T, 1><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+  else if (steps <= 2) expand_tile<T, 2><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+  else if (steps <= 4) expand_tile<T, 4><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+  else if constexpr (sizeof(T) == 4)
+    expand_tile<T, 8><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_lowrank(const LowrankArgs& a, hipStream_t s) {
+  float* h = reinterpret_cast<float*>(a.space);
+  if (a.tokens <= kFew) {
+    shrink_few<T><<<dim3((unsigned)a.tokens, (unsigned)(a.rank + 3) / 4u), 256, 0, s>>>(
+        static_cast<const T*>(a.x), a.x_stride, a.ids, static_cast<const T*>(a.down), h, a.tokens, a.inputs, a.rank,
+        a.adapters);
+    expand_few<T><<<dim3((unsigned)a.tokens, (unsigned)(a.outputs + 255) / 256u), 256, 0, s>>>(
+        h, a.ids, static_cast<const T*>(a.up), a.scale, static_cast<const T*>(a.base), a.base_stride,
+        static_cast<T*>(a.y), a.y_stride, a.outputs, a.rank, a.adapters);
+    return hipGetLastError();
+  }
+  const Shrink p{a.x, a.down, h, a.x_stride, a.inputs};
+  const hipError_t e = run_shrink<T>(p, p, 1, a, nullptr, s);
+  if (e != hipSuccess) return e;
+  return run_expand<T>(Expand{h, a.up, a.base, a.y, a.base_stride, a.y_stride, a.outputs}, a, s);
+}
+
+// The backward call's workspace.
+struct BackwardPlan {
+  int splits, blocks_down, blocks_up;
+  size_t h, g, down_t, up_t, range, part_down, part_up, bytes;
+};
+
+BackwardPlan plan_backward(const LowrankArgs& a, int size) {
+  BackwardPlan b;
+  const int cols = 16 * (16 / size);
+  b.blocks_down = (a.inputs + cols - 1) / cols;
+  b.blocks_up = (a.outputs + cols - 1) / cols;
+  // an adapter's tokens in parts: some 1024 workgroups, not under 64 tokens each
+  const int64_t cells = (int64_t)a.adapters * (b.blocks_down + b.blocks_up);
+  int64_t splits = (1024 + cells - 1) / cells;
+  const int64_t most = (a.tokens + 63) / 64;
+  b.splits = (int)(splits < most ? splits : most);
+  const size_t rows = (size_t)a.tokens * row_of(a.rank) * 4;
+  const size_t down = (size_t)a.adapters * a.rank * a.inputs, up = (size_t)a.adapters * a.rank * a.outputs;
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t was = at;
+    at += up64(n);
+    return was;
+  };
+  b.h = take(rows);
+  b.g = take(rows);
+  b.down_t = take(down * size);
+  b.up_t = take(up * size);
+  b.range = take((size_t)a.adapters * 8);
+  b.part_down = take(down * 4 * b.splits);
+  b.part_up = take(up * 4 * b.splits);
+  b.bytes = at;
+  return b;
+}
+
+template <typename T, int RT>
+void run_outer(const Outer& p0, const Outer& p1, const LowrankArgs& a, const int2* range, int splits, hipStream_t s) {
+  const dim3 grid((unsigned)((p0.blocks + p1.blocks) * a.adapters), (unsigned)splits, (unsigned)((a.rank + RT * 16 - 1) / (RT * 16)));
+  outer_tile<T, RT><<<grid, 256, 0, s>>>(p0, p1, a.ids, range, a.tokens, a.rank, a.adapters, splits);
+}
+
+template <typename T>
+hipError_t run_finish(const LowrankArgs& a, const float* part_down, const float* part_up, int splits, hipStream_t s) {
+  const int down = (a.inputs + 255) / 256, up = (a.outputs + 255) / 256;
+  const dim3 grid((unsigned)((down + up) * a.adapters), (unsigned)((a.rank + 3) / 4));
+  outer_finish<T><<<grid, 256, 0, s>>>(part_down, part_up, a.scale, static_cast<T*>(a.d_down), static_cast<T*>(a.d_up), a.rank,
+                                       a.inputs, a.outputs, a.adapters, splits, down, up);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_lowrank_backward(const LowrankArgs& a, hipStream_t s) {
+  const BackwardPlan b = plan_backward(a, (int)sizeof(T));
+  float* h = reinterpret_cast<float*>(a.space + b.h);
+  float* g = reinterpret_cast<float*>(a.space + b.g);
+  T* down_t = reinterpret_cast<T*>(a.space + b.down_t);
+  T* up_t = reinterpret_cast<T*>(a.space + b.up_t);
+  int2* range = reinterpret_cast<int2*>(a.space + b.range);
+  float* part_down = reinterpret_cast<float*>(a.space + b.part_down);
+  float* part_up = reinterpret_cast<float*>(a.space + b.part_up);
+  const int tiles_down = (a.rank + 63) / 64 * ((a.inputs + 63) / 64), tiles_up = (a.rank + 63) / 64 * ((a.outputs + 63) / 64);
+  transpose_banks<T><<<dim3((unsigned)((tiles_down + tiles_up) * a.adapters)), 256, 0, s>>>(
+      static_cast<const T*>(a.down), down_t, static_cast<const T*>(a.up), up_t, range, a.adapters, a.rank, a.inputs, a.outputs,
+      tiles_down, tiles_up);
+  // h = x down^T and g = dy up
+  hipError_t e = run_shrink<T>(Shrink{a.x, a.down, h, a.x_stride, a.inputs}, Shrink{a.dy, up_t, g, a.dy_stride, a.outputs}, 2,
+                               a, range, s);
+  if (e != hipSuccess) return e;
+  e = run_expand<T>(Expand{g, down_t, a.base, a.y, a.base_stride, a.y_stride, a.inputs}, a, s);
+  if (e != hipSuccess) return e;
+  const Outer p0{g, a.x, part_down, a.x_stride, a.inputs, b.blocks_down};
+  const Outer p1{h, a.dy, part_up, a.dy_stride, a.outputs, b.blocks_up};
+  if (a.rank <= 16) run_outer<T, 1>(p0, p1, a, range, b.splits, s);
+  else if (a.rank <= 32) run_outer<T, 2>(p0, p1, a, range, b.splits, s);
+  else run_outer<T, 4>(p0, p1, a, range, b.splits, s);
+  return run_finish<T>(a, part_down, part_up, b.splits, s);
+}
+
+// Sums over nothing.
+template <typename T>
+hipError_t run_no_tokens(const LowrankArgs& a, hipStream_t s) {
+  return run_finish<T>(a, nullptr, nullptr, 0, s);
+}
+
+}  // namespace
+
+size_t lowrank_bytes(const LowrankArgs& a) { return (size_t)a.tokens * row_of(a.rank) * 4; }
+
+size_t lowrank_backward_bytes(const LowrankArgs& a, int size) { return plan_backward(a, size).bytes; }
+
+hipError_t launch_lowrank(const LowrankArgs& a, int type, hipStream_t s) {
+  if (type == 0) return run_lowrank<float>(a, s);
+  return type == 1 ? run_lowrank<f16>(a, s) : run_lowrank<bf16>(a, s);
+}
+
+hipError_t launch_lowrank_no_tokens(const LowrankArgs& a, int type, hipStream_t s) {
+  if (type == 0) return run_no_tokens<float>(a, s);
+  return type == 1 ? run_no_tokens<f16>(a, s) : run_no_tokens<bf16>(a, s);
+}
+
+hipError_t launch_lowrank_backward(const LowrankArgs& a, int type, hipStream_t s) {
+  if (type == 0) return run_lowrank_backward<float>(a, s);
+  return type == 1 ? run_lowrank_backward<f16>(a, s) : run_lowrank_backward<bf16>(a, s);
+}
+
+}  // namespace sfc

@@ -1,0 +1,109 @@
+// C entry points of the low-rank adapters: checks and workspace sizes.
+#include "sfc.h"
+#include "sfc_lowrank.hpp"
+
+namespace {
+
+using sfc::LowrankArgs;
+
+bool aligned(const void* p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
+
+sfc_status describe(const sfc_lowrank_desc* d, LowrankArgs* a) {
+  if (!d) return SFC_EINVAL;
+  if (d->tokens < 0 || d->inputs <= 0 || d->outputs <= 0 || d->rank <= 0 || d->adapters <= 0) return SFC_EINVAL;
+  if (d->type < SFC_TYPE_F32 || d->type > SFC_TYPE_BF16) return SFC_EINVAL;
+  if (d->tokens > 1 << 26 || d->inputs > 1 << 20 || d->outputs > 1 << 20 || d->rank > 128 || d->adapters > 1 << 16)
+    return SFC_EUNSUPPORTED;
+  *a = LowrankArgs{};
+  a->tokens = (int)d->tokens;
+  a->inputs = d->inputs;
+  a->outputs = d->outputs;
+  a->rank = d->rank;
+  a->adapters = d->adapters;
+  a->x_stride = d->x_stride ? d->x_stride : d->inputs;
+  if (a->x_stride < d->inputs || a->x_stride > (int64_t)1 << 32) return SFC_EINVAL;
+  return SFC_OK;
+}
+
+// Strides of rows of `length`, 0: dense.
+bool stride_of(int64_t asked, int length, int64_t* stride) {
+  *stride = asked ? asked : length;
+  return *stride >= length && *stride <= (int64_t)1 << 32;
+}
+
+}  // namespace
+
+extern "C" {
+
+sfc_status sfc_lowrank_sizes(const sfc_lowrank_desc* desc, size_t* forward_bytes, size_t* backward_bytes) {
+  LowrankArgs a;
+  const sfc_status st = describe(desc, &a);
+  if (st != SFC_OK) return st;
+  if (forward_bytes) *forward_bytes = sfc::lowrank_bytes(a);
+  if (backward_bytes)
+    *backward_bytes = a.tokens ? sfc::lowrank_backward_bytes(a, desc->type == SFC_TYPE_F32 ? 4 : 2) : 0;
+  return SFC_OK;
+}
+
+sfc_status sfc_lowrank_add(const sfc_lowrank_desc* desc, const void* x_dev, const int32_t* ids_dev,
+                           const void* down_dev, const void* up_dev, const float* scale_dev, const void* base_dev,
+                           void* y_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  LowrankArgs a;
+  const sfc_status st = describe(desc, &a);
+  if (st != SFC_OK) return st;
+  if (!stride_of(desc->base_stride, desc->outputs, &a.base_stride) || !stride_of(desc->y_stride, desc->outputs, &a.y_stride))
+    return SFC_EINVAL;
+  if (a.tokens == 0) return SFC_OK;
+  if (!x_dev || !ids_dev || !down_dev || !up_dev || !y_dev) return SFC_EINVAL;
+  const int size = desc->type == SFC_TYPE_F32 ? 4 : 2;
+  if (!aligned(x_dev, size) || !aligned(ids_dev, 4) || !aligned(down_dev, size) || !aligned(up_dev, size) ||
+      !aligned(scale_dev, 4) || !aligned(base_dev, size) || !aligned(y_dev, size) || !aligned(workspace_dev, 16))
+    return SFC_EINVAL;
+  if (!workspace_dev || workspace_bytes < sfc::lowrank_bytes(a)) return SFC_EWORKSPACE;
+  a.x = x_dev;
+  a.ids = ids_dev;
+  a.down = down_dev;
+  a.up = up_dev;
+  a.scale = scale_dev;
+  a.base = base_dev;
+  a.y = y_dev;
+  a.space = static_cast<char*>(workspace_dev);
+  return sfc::launch_lowrank(a, desc->type, static_cast<hipStream_t>(stream)) == hipSuccess ? SFC_OK : SFC_EHIP;
+}
+
+sfc_status sfc_lowrank_backward(const sfc_lowrank_desc* desc, const void* x_dev, const void* dy_dev,
+                                const int32_t* ids_dev, const void* down_dev, const void* up_dev,
+                                const float* scale_dev, const void* dx_base_dev, void* dx_dev, void* d_down_dev,
+                                void* d_up_dev, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  LowrankArgs a;
+  const sfc_status st = describe(desc, &a);
+  if (st != SFC_OK) return st;
+  if (!stride_of(desc->y_stride, desc->outputs, &a.dy_stride) || !stride_of(desc->base_stride, desc->inputs, &a.base_stride) ||
+      !stride_of(desc->dx_stride, desc->inputs, &a.y_stride))
+    return SFC_EINVAL;
+  const int size = desc->type == SFC_TYPE_F32 ? 4 : 2;
+  if (!d_down_dev || !d_up_dev || !aligned(d_down_dev, size) || !aligned(d_up_dev, size) || !aligned(scale_dev, 4))
+    return SFC_EINVAL;
+  a.d_down = d_down_dev;
+  a.d_up = d_up_dev;
+  a.scale = scale_dev;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (a.tokens == 0)
+    return sfc::launch_lowrank_no_tokens(a, desc->type, s) == hipSuccess ? SFC_OK : SFC_EHIP;
+  if (!x_dev || !dy_dev || !ids_dev || !down_dev || !up_dev || !dx_dev) return SFC_EINVAL;
+  if (!aligned(x_dev, size) || !aligned(dy_dev, size) || !aligned(ids_dev, 4) || !aligned(down_dev, size) ||
+      !aligned(up_dev, size) || !aligned(dx_base_dev, size) || !aligned(dx_dev, size) || !aligned(workspace_dev, 16))
+    return SFC_EINVAL;
+  if (!workspace_dev || workspace_bytes < sfc::lowrank_backward_bytes(a, size)) return SFC_EWORKSPACE;
+  a.x = x_dev;
+  a.dy = dy_dev;
+  a.ids = ids_dev;
+  a.down = down_dev;
+  a.up = up_dev;
+  a.base = dx_base_dev;
+  a.y = dx_dev;
+  a.space = static_cast<char*>(workspace_dev);
+  return sfc::launch_lowrank_backward(a, desc->type, s) == hipSuccess ? SFC_OK : SFC_EHIP;
+}
+
+}  // extern "C"

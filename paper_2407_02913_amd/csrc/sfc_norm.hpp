@@ -117,26 +117,6 @@ __device__ __forceinline__ void activate_back(int activation, const float (&z)[V
   }
 }
 
-// Loaded vectors behind whose last valid element may lie others of the same tensor: read whole unless the
-// tensor ends, cut to the valid ones.
-template <typename T>
-__device__ __forceinline__ raw4 load_cut(const T* p, int valid, int64_t room) {
-  if (valid >= kVec<T>) return load16(p);
-  if (room < kVec<T>) return load_part(p, valid);
-  raw4 r = load16(p);
-  constexpr int per = 4 / (int)sizeof(T);
-#pragma unroll
-  for (int d = 0; d < 4; ++d) {
-    if constexpr (per == 1) {
-      if (d >= valid) r[d] = 0u;
-    } else {
-      if (2 * d >= valid) r[d] = 0u;
-      else if (2 * d + 1 >= valid) r[d] &= 0xffffu;
-    }
-  }
-  return r;
-}
-
 // int8 activations of the next convolution: round-half-even(v * inv) within +-127 (quantize_byte's way).
 template <int V>
 __device__ __forceinline__ void store_i8(int8_t* p, const float (&v)[V], float inv, int valid) {

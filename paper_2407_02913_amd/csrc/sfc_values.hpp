@@ -41,6 +41,25 @@ __device__ __forceinline__ raw4 load_part(const T* p, int valid) {
   return r;
 }
 
+// The first `valid` elements at p and `fill` behind them; `room` elements lie between p and the end of the tensor,
+// and the vector is read whole unless it ends before.
+template <typename T>
+__device__ __forceinline__ raw4 load_cut(const T* p, int valid, int64_t room, unsigned fill = 0u) {
+  if (valid >= kVec<T>) return load16(p);
+  raw4 r = room < kVec<T> ? load_part(p, valid) : load16(p);
+  constexpr int per = 4 / (int)sizeof(T);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (per == 1) {
+      if (d >= valid) r[d] = fill;
+    } else {
+      if (2 * d >= valid) r[d] = fill;
+      else if (2 * d + 1 >= valid) r[d] = (r[d] & 0xffffu) | (fill & 0xffff0000u);
+    }
+  }
+  return r;
+}
+
 // Element j of a loaded vector as a float.
 template <typename T>
 __device__ __forceinline__ float element(const raw4& r, int j) {

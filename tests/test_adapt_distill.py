@@ -1,0 +1,297 @@
+"""Distillation from a teacher's top logits against its definition in 64 bits: rows in a wave, in a workgroup and past
+the registers, odd class counts, padding, places given twice, masked and empty rows, infinities, strides, refusals.
+
+Tolerances, set before the first run.  A loss is a sum of p (log p - log q): logarithms and arguments of exponentials
+up to some tens carry 2^-24 of themselves, so 2e-6 times the sum of p (|log p| + |log q|) + 1e-6, times T^2.  A
+gradient's q has the relative error of its exponential, 2^-23 (|argument| + 4), at most 1e-5 for arguments to 60; both
+terms together 1e-5 (q + p) of the row's scale, plus half a step of its type."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+# rows, classes, top
+SHAPES = [
+    (1, 1, 1), (3, 2, 1), (5, 10, 3), (64, 1000, 10), (7, 255, 255), (9, 1024, 64), (6, 2049, 33), (13, 4099, 100),
+    (4, 8200, 65), (5, 16385, 7), (3, 32003, 33), (3, 50001, 128), (2, 65537, 1024), (2, 131072, 64), (2, 131081, 40),
+    (1, 262144, 64),
+]
+
+
+def definition(logits, values, index, temperature, tail):
+    """(loss, dloss/dlogits, magnitude of the loss's terms, q, p at every class) in 64 bits."""
+    rows, classes = logits.shape
+    z = logits.double() / temperature
+    log_q = torch.log_softmax(z, 1)
+    q = log_q.exp()
+    there = (index >= 0) & (index < classes)
+    at = torch.where(there, index, 0).long()
+    if tail:
+        log_p = values.double()
+    else:
+        log_p = torch.log_softmax(torch.where(there, values.double(), -math.inf) / temperature, 1)
+    p = torch.where(there, log_p.exp(), 0.0)
+    p = torch.where(there.any(1, keepdim=True), p, 0.0)
+    lq = log_q.gather(1, at)
+    term = torch.where(p > 0, p * (log_p - lq), 0.0)
+    size = torch.where(p > 0, p * (log_p.abs() + lq.abs()), 0.0).sum(1)
+    loss = term.sum(1)
+    dense = torch.zeros_like(q).scatter_add(1, at, p)
+    grad = q * p.sum(1, keepdim=True) - dense
+    if tail:
+        inside = torch.zeros_like(q).scatter_add(1, at, there.double()) > 0
+        p_rest = (1 - p.sum(1)).clamp(min=0)
+        q_rest = torch.where(inside, 0.0, q).sum(1)
+        real = (p_rest > 1e-6) | ((q_rest > 0) & (p_rest > 0))
+        rest = torch.where(real, p_rest * (p_rest.log() - q_rest.log()), 0.0)
+        loss = loss + rest
+        size = size + torch.where(real, p_rest * (p_rest.log().abs() + q_rest.log().abs()), 0.0)
+        ratio = torch.where(real, p_rest / q_rest, 0.0)
+        share = torch.where(real, p_rest, 0.0)
+        grad = grad + q * share.view(-1, 1) - torch.where(inside, 0.0, q) * ratio.view(-1, 1)
+        dense = dense + torch.where(inside, 0.0, q) * ratio.view(-1, 1)
+    t = temperature
+    return loss * t * t, grad * t, size * t * t, q, dense
+
+
+def make(shape, dtype, tail, seed=0, twice=False, pad=False):
+    rows, classes, top = shape
+    g = torch.Generator().manual_seed(seed)
+    logits = torch.randn(rows, classes, generator=g) * 3
+    index = torch.stack([torch.randperm(classes, generator=g)[:top] for _ in range(rows)]).to(torch.int64)
+    values = torch.randn(rows, top, generator=g) * 2 + 3
+    if tail:
+        # (where the places are all classes nothing is left but rounding)
+        values = torch.log_softmax(values, 1) + (math.log(0.8) if top < classes else 0.0)
+    if twice and top > 2:
+        index[:, 1] = index[:, 0]
+    if pad:
+        index[:, top // 2] = -1
+        index[0, :] = -1  # a row without a teacher
+        if rows > 2:
+            index[2, 0] = classes  # past the last class
+    row_scale = torch.rand(rows, generator=g) + 0.25
+    if rows > 1:
+        row_scale[rows // 2] = 0.0
+    return logits.to(dtype).cuda(), values.cuda(), index.cuda(), row_scale.cuda()
+
+
+def check(got, want, dtype, row_scale, temperature):
+    loss, grad = got
+    ref_loss, ref_grad, size, q, p = want
+    kept = row_scale != 0
+    assert ((loss.double() - ref_loss).abs() <= 2e-6 * size + 1e-6 * temperature ** 2)[kept].all()
+    assert (loss[~kept] == 0).all() and (grad[~kept] == 0).all()
+    scale = row_scale.double().view(-1, 1)
+    ref = ref_grad * scale
+    tol = 1e-5 * (q + p) * scale * temperature + STEP[dtype] * ref.abs() + 2.0 ** -25
+    assert ((grad.double() - ref).abs() <= tol)[kept].all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tail", [False, True])
+def test_loss_and_gradient(shape, dtype, tail):
+    from paper_2407_02913_amd import adapt
+
+    for temperature, twice, pad in ((1.0, False, False), (2.5, True, False), (0.7, False, True)):
+        if tail and twice:
+            continue  # (log-probabilities of one class given twice mean nothing)
+        print("distill", shape, dtype, tail, temperature, flush=True)
+        logits, values, index, row_scale = make(shape, dtype, tail, 1, twice, pad)
+        how = {"row_scale": row_scale, "temperature": temperature, "tail": tail}
+        want = definition(logits, values, index, temperature, tail)
+        both = adapt.distill_loss_and_grad(logits, values, index.to(torch.int32), **how)
+        check(both, want, dtype, row_scale, temperature)
+        loss, stats = adapt.distill_loss(logits, values, index, **how)
+        grad = adapt.distill_grad(logits, values, index, stats, **how)
+        check((loss, grad), want, dtype, row_scale, temperature)
+        assert grad.dtype == dtype and torch.equal(loss, both[0])
+        # the gradient in place of the logits, and the same bits again
+        again = logits.clone()
+        adapt.distill_loss_and_grad(again, values, index, out=again, **how)
+        assert torch.equal(again, both[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("classes", [37, 1000, 20011, 140001])
+def test_gradient_against_differences(classes, tail):
+    """Differences of the 64-bit loss in a random direction, through autograd's entry."""
+    from paper_2407_02913_amd import adapt
+
+    logits, values, index, _ = make((4, classes, 9), torch.float32, tail, 2)
+    mask = torch.tensor([1.0, 0.0, 1.0, 1.0], device="cuda")
+    logits.requires_grad_(True)
+    loss = adapt.distill(logits, values, index, mask, 1.5, tail)
+    weight = torch.tensor([0.5, 3.0, -1.0, 2.0], device="cuda")
+    grad, = torch.autograd.grad((loss * weight).sum(), logits)
+    at = logits.detach().double()
+    v = torch.randn(at.shape, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").double()
+    total = lambda x: float((definition(x, values, index, 1.5, tail)[0] * weight * mask).sum())  # noqa: E731
+    difference = (total(at + 1e-4 * v) - total(at - 1e-4 * v)) / 2e-4
+    slope = float((grad.double() * v).sum())
+    # the gradient's rounding (1e-5 of its terms) and the differences' third order (1e-8)
+    terms = float((definition(at, values, index, 1.5, tail)[3] * v.abs()).sum()) * 10 + 10
+    assert abs(slope - difference) <= 1e-5 * terms + 1e-5
+    assert (grad[1] == 0).all() and loss[1] == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("classes", [50, 5000, 140001])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_and_nan(classes, dtype):
+    """Classes masked with -inf or the type's lowest value; a NaN or +inf breaks its own row; a masked row's values
+    are not looked at."""
+    from paper_2407_02913_amd import adapt
+
+    for tail in (False, True):
+        logits, values, index, _ = make((6, classes, 8), dtype, tail, 4)
+        lowest = torch.finfo(dtype).min
+        outside = torch.ones(6, classes, dtype=torch.bool, device="cuda").scatter(1, index, False)
+        drop = outside & (torch.rand(6, classes, device="cuda") < 0.5)
+        logits[0] = torch.where(drop[0], -math.inf, logits[0].float()).to(dtype)
+        logits[1] = torch.where(drop[1], torch.tensor(lowest, dtype=dtype, device="cuda"), logits[1])
+        logits[2, index[2, 0]] = math.nan
+        logits[3] = math.nan  # masked
+        logits[4, index[4, 1]] = math.inf
+        if not tail:
+            values[5, 3] = -math.inf  # a teacher's entry without mass
+            logits[5, index[5, 3]] = -math.inf
+        row_scale = torch.tensor([1.0, 1.0, 1.0, 0.0, 1.0, 1.0], device="cuda")
+        loss, grad = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=1.25, tail=tail)
+        rows = [0, 1, 5]
+        want = definition(logits[rows], values[rows], index[rows], 1.25, tail)
+        check((loss[rows], grad[rows]), want, dtype, row_scale[rows], 1.25)
+        assert loss[3] == 0 and (grad[3] == 0).all()
+        for r in (2, 4):
+            assert torch.isnan(loss[r]) and torch.isnan(grad[r]).all()
+        # the teacher's place at -inf with mass: the loss is infinite, the gradient finite
+        logits[0, index[0, 0]] = -math.inf
+        loss, grad = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=1.25, tail=tail)
+        assert loss[0] == math.inf and torch.isfinite(grad[0]).all()
+        logits[1] = -math.inf
+        loss, grad = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=1.25, tail=tail)
+        assert torch.isnan(loss[1]) and torch.isnan(grad[1]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("classes", [600, 20000])
+def test_the_rest_of_a_certain_student(classes):
+    """A student who has all but 1e-9 of its mass on the top: the rest is summed as such, not as a difference."""
+    from paper_2407_02913_amd import adapt
+
+    logits, values, index, _ = make((3, classes, 4), torch.float32, True, 5)
+    logits = logits.scatter(1, index, 30.0 + torch.arange(4, device="cuda").float().expand(3, 4))
+    ones = torch.ones(3, device="cuda")
+    got = adapt.distill_loss_and_grad(logits, values, index, temperature=1.0, tail=True)
+    check(got, definition(logits, values, index, 1.0, True), torch.float32, ones, 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_strides_streams_graphs_and_nothing(dtype):
+    from paper_2407_02913_amd import adapt
+
+    logits, values, index, row_scale = make((9, 5003, 12), dtype, False, 6)
+    want = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=2.0)
+    wide = torch.zeros(9, 5003 + 14, dtype=dtype, device="cuda")
+    view = wide[:, 3:3 + 5003]
+    view.copy_(logits)
+    wide_values, wide_index = torch.zeros(9, 20, device="cuda"), torch.zeros(9, 17, dtype=torch.int64, device="cuda")
+    wide_values[:, 2:14], wide_index[:, 1:13] = values, index
+    got = adapt.distill_loss_and_grad(view, wide_values[:, 2:14], wide_index[:, 1:13], row_scale=row_scale, temperature=2.0,
+                                      out=view)
+    assert torch.equal(got[0], want[0]) and torch.equal(view, want[1])
+    assert (wide[:, :3] == 0).all() and (wide[:, 3 + 5003:] == 0).all()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=2.0)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=2.0)
+    for k in range(3):
+        logits.copy_(make((9, 5003, 12), dtype, False, 20 + k)[0])
+        want = adapt.distill_loss_and_grad(logits, values, index, row_scale=row_scale, temperature=2.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    none = adapt.distill_loss_and_grad(logits[:0], values[:0], index[:0])
+    assert none[0].shape == (0,) and none[1].shape == (0, 5003)
+    # no scales: ones
+    a = adapt.distill_loss_and_grad(logits, values, index)
+    b = adapt.distill_loss_and_grad(logits, values, index, row_scale=torch.ones(9, device="cuda"))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def _desc(**kw):
+    from paper_2407_02913_amd import binding
+
+    d = dict(rows=4, classes=100, top=5, type=0, index_wide=0, tail=0, temperature=1.0, logits_stride=0, grad_stride=0,
+             values_stride=0, index_stride=0)
+    d.update(kw)
+    return binding.DistillDesc(**d)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"rows": -1}, 1), ({"classes": 0}, 1), ({"top": 0}, 1), ({"type": 3}, 1), ({"type": -1}, 1), ({"index_wide": 2}, 1),
+    ({"tail": -1}, 1), ({"temperature": 0.0}, 1), ({"temperature": math.nan}, 1), ({"temperature": math.inf}, 1),
+    ({"logits_stride": 99}, 1), ({"grad_stride": 5}, 1), ({"values_stride": 4}, 1), ({"index_stride": -1}, 1),
+    ({"classes": (1 << 18) + 1}, 2), ({"top": 1025}, 2), ({"rows": 1 << 31}, 2),
+])
+def test_bad_descriptions(kw, code):
+    """Refused before any launch: no GPU is needed."""
+    from paper_2407_02913_amd import binding
+
+    lib, d = binding.load(), _desc(**kw)
+    at = C.addressof(d)
+    assert lib.sfc_distill_loss_grad(at, 256, 256, 256, 256, 256, 256, None) == code
+    assert lib.sfc_distill_loss(at, 256, 256, 256, 256, 256, 256, None) == code
+    assert lib.sfc_distill_grad(at, 256, 256, 256, 256, 256, 256, None) == code
+
+
+def test_bad_pointers():
+    from paper_2407_02913_amd import binding
+
+    lib, d = binding.load(), _desc()
+    at = C.addressof(d)
+    assert lib.sfc_distill_loss_grad(None, 256, 256, 256, 256, 256, 256, None) == 1
+    for missing in (1, 2, 3, 5, 6):
+        args = [at, 256, 256, 256, 256, 256, 256, None]
+        args[missing] = None
+        assert lib.sfc_distill_loss_grad(*args) == 1, missing
+    for odd in (1, 2, 3, 4, 5, 6):
+        args = [at, 256, 256, 256, 256, 256, 256, None]
+        args[odd] = 257
+        assert lib.sfc_distill_loss_grad(*args) == 1, odd
+    assert lib.sfc_distill_loss(at, 256, 256, 256, 256, None, 256, None) == 1
+    assert lib.sfc_distill_grad(at, 256, 256, 256, 256, None, 256, None) == 1
+    assert lib.sfc_distill_grad(at, 256, 256, 256, 256, 264, 256, None) == 1
+    assert lib.sfc_distill_loss_grad(C.addressof(_desc(rows=0)), None, None, None, None, None, None, None) == 0
+
+
+@pytest.mark.gpu
+def test_bad_tensors():
+    from paper_2407_02913_amd import adapt, binding
+
+    logits, values, index, scale = make((4, 50, 5), torch.float32, False)
+    for bad in ((logits.cpu(), values, index), (logits[0], values, index), (logits.double(), values, index),
+                (logits, values.half(), index), (logits, values[:2], index), (logits, values, index.float()),
+                (logits, values, index[:, :3]), (logits.t().contiguous().t(), values, index)):
+        with pytest.raises(ValueError):
+            adapt.distill_loss(*bad)
+    with pytest.raises(ValueError):
+        adapt.distill_loss(logits, values, index, row_scale=scale[:2])
+    with pytest.raises(ValueError):
+        adapt.distill_loss_and_grad(logits, values, index, out=logits.half())
+    with pytest.raises(binding.SfcError):
+        adapt.distill_loss(logits, values, index, temperature=0.0)
+    _, stats = adapt.distill_loss(logits, values, index)
+    with pytest.raises(ValueError):
+        adapt.distill_grad(logits, values, index, stats[:2])

@@ -1,0 +1,290 @@
+"""Low-rank adapters of many requests against their definition in 64 bits: single tokens and tiles, counts that fill no
+vector and no tile, runs and mixtures of adapters, tokens without one, broken adapters, strides, gradients, refusals.
+
+Tolerances, set before the first run: sums in 32 bits are off by 4e-6 of the sum of their terms' magnitudes (2^-24 times
+some tens, the partial sums of a few thousand terms being far smaller than that sum); bfloat16 keeps 16 bits of h in the
+second product (2^-16 of its terms' magnitudes); results in 16 bits add half a step of their type."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+# tokens, inputs, outputs, rank, adapters
+SHAPES = [
+    (1, 1, 1, 1, 1), (1, 512, 1000, 8, 4), (3, 17, 5, 3, 2), (64, 300, 260, 16, 64), (256, 64, 64, 5, 3),
+    (257, 64, 64, 16, 1), (300, 129, 257, 17, 3), (511, 1000, 333, 33, 2), (700, 333, 1000, 64, 5), (290, 96, 130, 65, 2),
+    (1030, 40, 72, 128, 3), (2051, 520, 264, 12, 4), (400, 31, 9, 100, 2),
+]
+
+
+def make(shape, dtype, seed=0, runs=True):
+    t, k, m, r, a = shape
+    g = torch.Generator().manual_seed(seed)
+    normal = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).to(dtype).cuda()  # noqa: E731
+    ids = torch.randint(-1, a, (t,), generator=g)
+    if runs:
+        ids = ids.sort()[0]
+        ids[t // 3: t // 3 + 2] = a  # none
+    return {"x": normal(t, k), "base": normal(t, m), "down": normal(a, r, k, scale=k ** -0.5),
+            "up": normal(a, m, r, scale=r ** -0.5), "scale": (torch.rand(a, generator=g) + 0.5).cuda(),
+            "ids": ids.to(torch.int32).cuda(), "dy": normal(t, m), "dx_base": normal(t, k)}
+
+
+def definition(d, ids, with_scale=True):
+    """y, dx, d_down, d_up in 64 bits, and the sums of the magnitudes of what each is made of."""
+    x, dy, down, up = (d[n].double() for n in ("x", "dy", "down", "up"))
+    out = {"y": d["base"].double().clone(), "dx": d["dx_base"].double().clone(), "d_down": torch.zeros_like(down),
+           "d_up": torch.zeros_like(up)}
+    size = {n: v.abs() for n, v in out.items()}
+    second = {n: torch.zeros_like(v) for n, v in out.items()}  # terms of the products with h or g alone
+    for l in range(down.shape[0]):
+        at = torch.nonzero(ids == l)[:, 0]
+        s = float(d["scale"][l]) if with_scale else 1.0
+        h, g = x[at] @ down[l].t(), dy[at] @ up[l]
+        ha, ga = x[at].abs() @ down[l].abs().t(), dy[at].abs() @ up[l].abs()
+        out["y"][at] += s * (h @ up[l].t())
+        size["y"][at] += s * (ha @ up[l].abs().t())
+        second["y"][at] += s * (h.abs() @ up[l].abs().t())
+        out["dx"][at] += s * (g @ down[l])
+        size["dx"][at] += s * (ga @ down[l].abs())
+        second["dx"][at] += s * (g.abs() @ down[l].abs())
+        out["d_down"][l] = s * (g.t() @ x[at])
+        size["d_down"][l] = s * (ga.t() @ x[at].abs())
+        out["d_up"][l] = s * (dy[at].t() @ h)
+        size["d_up"][l] = s * (dy[at].abs().t() @ ha)
+    return out, size, second
+
+
+def near(got, name, want, dtype):
+    out, size, second = want
+    tol = 4e-6 * size[name] + STEP[dtype] * out[name].abs() + 2.0 ** -25
+    if dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -16 * second[name]
+    assert got.dtype == dtype and got.shape == out[name].shape
+    worst = ((got.double() - out[name]).abs() - tol).max() if got.numel() else torch.tensor(-1.0)
+    assert worst <= 0, (name, float(worst))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("runs", [True, False])
+def test_forward_and_backward(shape, dtype, runs):
+    from paper_2407_02913_amd import adapt
+
+    print("lowrank", shape, dtype, runs, flush=True)
+    d = make(shape, dtype, 1, runs)
+    want = definition(d, d["ids"])
+    bank = d["ids"], d["down"], d["up"], d["scale"]
+    near(adapt.add_adapters(d["base"], d["x"], *bank), "y", want, dtype)
+    dx, d_down, d_up = adapt.add_adapters_backward(d["dy"], d["x"], *bank, dx_base=d["dx_base"])
+    near(dx, "dx", want, dtype)
+    near(d_down, "d_down", want, dtype)
+    near(d_up, "d_up", want, dtype)
+    # in place of the base; no base; no scales
+    y = d["base"].clone()
+    assert adapt.add_adapters(y, d["x"], *bank, out=y) is y
+    assert torch.equal(y, adapt.add_adapters(d["base"], d["x"], *bank))
+    bare = dict(d, base=torch.zeros_like(d["base"]), dx_base=torch.zeros_like(d["dx_base"]))
+    want = definition(bare, d["ids"], with_scale=False)
+    near(adapt.add_adapters(None, d["x"], *bank[:3]), "y", want, dtype)
+    near(adapt.add_adapters_backward(d["dy"], d["x"], *bank[:3])[0], "dx", want, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [40, 600])
+def test_requests_do_not_touch_each_other(dtype, tokens):
+    """An adapter or a token full of infinities and NaN changes nothing of the others, next to it in one tile."""
+    from paper_2407_02913_amd import adapt
+
+    d = make((tokens, 200, 300, 20, 4), dtype, 2, runs=False)
+    bank = d["ids"], d["down"], d["up"], d["scale"]
+    clean = adapt.add_adapters(d["base"], d["x"], *bank)
+    clean_back = adapt.add_adapters_backward(d["dy"], d["x"], *bank)
+    for value in (math.inf, math.nan):
+        broken = {k: v.clone() for k, v in d.items()}
+        broken["down"][1] = value
+        broken["up"][1] = value
+        bad = d["ids"] == 1
+        token = int(torch.nonzero(d["ids"] == 2)[0])
+        broken["x"][token] = value
+        bad[token] = True
+        bank = d["ids"], broken["down"], broken["up"], d["scale"]
+        y = adapt.add_adapters(d["base"], broken["x"], *bank)
+        assert torch.equal(y[~bad], clean[~bad]) and not torch.isfinite(y[bad]).any()
+        dx, d_down, d_up = adapt.add_adapters_backward(d["dy"], broken["x"], *bank)
+        of_adapter = d["ids"] == 1
+        assert torch.equal(dx[~of_adapter], clean_back[0][~of_adapter])
+        for l in (0, 3):
+            assert torch.equal(d_down[l], clean_back[1][l]) and torch.equal(d_up[l], clean_back[2][l])
+    none = torch.full_like(d["ids"], -1)
+    assert torch.equal(adapt.add_adapters(d["base"], d["x"], none, *bank[1:]), d["base"])
+    dx, d_down, d_up = adapt.add_adapters_backward(d["dy"], d["x"], none, *bank[1:], dx_base=d["dx_base"])
+    assert torch.equal(dx, d["dx_base"]) and (d_down == 0).all() and (d_up == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens", [50, 900])
+def test_float16_beyond_its_range_between_the_products(tokens):
+    """h of some 10^5, past float16, with an output within it."""
+    from paper_2407_02913_amd import adapt
+
+    d = make((tokens, 400, 96, 8, 2), torch.float16, 3)
+    d["down"] *= 2000
+    d["up"] *= 2.0 ** -14
+    want = definition(d, d["ids"])
+    bank = d["ids"], d["down"], d["up"], d["scale"]
+    y = adapt.add_adapters(d["base"], d["x"], *bank)
+    out, size, _ = want
+    assert ((y.double() - out["y"]).abs() <= 4e-6 * size["y"] + 2.0 ** -11 * out["y"].abs() + 2.0 ** -24).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tokens", [30, 500])
+def test_strides(dtype, tokens):
+    from paper_2407_02913_amd import adapt
+
+    d = make((tokens, 130, 77, 9, 3), dtype, 4)
+    bank = d["ids"], d["down"], d["up"], d["scale"]
+    y = adapt.add_adapters(d["base"], d["x"], *bank)
+    back = adapt.add_adapters_backward(d["dy"], d["x"], *bank, dx_base=d["dx_base"])
+
+    def wide(v, left, right):
+        w = torch.full((v.shape[0], v.shape[1] + left + right), 5.0, dtype=dtype, device="cuda")
+        w[:, left:left + v.shape[1]] = v
+        return w, w[:, left:left + v.shape[1]]
+
+    _, x = wide(d["x"], 3, 8)
+    whole, base = wide(d["base"], 1, 6)
+    _, dy = wide(d["dy"], 5, 0)
+    _, dx_base = wide(d["dx_base"], 0, 3)
+    adapt.add_adapters(base, x, *bank, out=base)
+    assert torch.equal(base, y) and (whole[:, :1] == 5).all() and (whole[:, 78:] == 5).all()
+    for a, b in zip(back, adapt.add_adapters_backward(dy, x, *bank, dx_base=dx_base)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences():
+    """Directional differences of the 64-bit sum(y dy), through autograd's entry."""
+    from paper_2407_02913_amd import adapt
+
+    d = make((333, 90, 70, 6, 3), torch.float32, 5)
+    names = ["base", "x", "down", "up"]
+    leaves = [d[n].requires_grad_(True) for n in names]
+    y = adapt.adapters(d["base"], d["x"], d["ids"], d["down"], d["up"], d["scale"])
+    grads = torch.autograd.grad(y, leaves, d["dy"])
+    at = {n: v.detach() for n, v in d.items()}
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for name, grad in zip(names, grads):
+        v = torch.randn(grad.shape, generator=g, device="cuda").double()
+        loss = lambda e: float((definition({**at, name: at[name].double() + e * v}, at["ids"])[0]["y"] * at["dy"].double()).sum())  # noqa: E731
+        # y is linear in each of them: a difference has no error of its own but rounding
+        difference = (loss(0.5) - loss(-0.5))
+        assert abs(float((grad.double() * v).sum()) - difference) <= 1e-5 * float((grad.double().abs() * v.abs()).sum()) + 1e-4
+
+
+@pytest.mark.gpu
+def test_nothing_repeats_streams_and_graphs():
+    from paper_2407_02913_amd import adapt
+
+    d = make((700, 264, 200, 24, 3), torch.bfloat16, 6)
+    bank = d["ids"], d["down"], d["up"], d["scale"]
+    y = adapt.add_adapters(d["base"][:0], d["x"][:0], d["ids"][:0], *bank[1:])
+    assert y.shape == (0, 200)
+    dx, d_down, d_up = adapt.add_adapters_backward(d["dy"][:0], d["x"][:0], d["ids"][:0], *bank[1:])
+    assert dx.shape == (0, 264) and (d_down == 0).all() and (d_up == 0).all()
+
+    def step():
+        return (adapt.add_adapters(d["base"], d["x"], *bank),
+                *adapt.add_adapters_backward(d["dy"], d["x"], *bank, dx_base=d["dx_base"]))
+
+    first = step()
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(first, step()))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = step()
+    for k in range(3):
+        d["x"].copy_(make((700, 264, 200, 24, 3), torch.bfloat16, 30 + k)["x"])
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def _desc(**kw):
+    from paper_2407_02913_amd import binding
+
+    d = dict(tokens=300, inputs=64, outputs=48, rank=8, adapters=3, type=0, x_stride=0, base_stride=0, y_stride=0, dx_stride=0)
+    d.update(kw)
+    return binding.LowrankDesc(**d)
+
+
+@pytest.mark.parametrize("kw,code", [
+    ({"tokens": -1}, 1), ({"inputs": 0}, 1), ({"outputs": -3}, 1), ({"rank": 0}, 1), ({"adapters": 0}, 1), ({"type": 3}, 1),
+    ({"type": -1}, 1), ({"x_stride": 63}, 1), ({"rank": 129}, 2), ({"adapters": (1 << 16) + 1}, 2),
+    ({"tokens": (1 << 26) + 1}, 2), ({"inputs": (1 << 20) + 1}, 2), ({"outputs": (1 << 20) + 1}, 2),
+])
+def test_bad_descriptions(kw, code):
+    """Refused before any launch: no GPU is needed."""
+    from paper_2407_02913_amd import binding
+
+    lib, d, big = binding.load(), _desc(**kw), 1 << 40
+    at = C.addressof(d)
+    assert lib.sfc_lowrank_sizes(at, None, None) == code
+    assert lib.sfc_lowrank_add(at, *[256] * 8, big, None) == code
+    assert lib.sfc_lowrank_backward(at, *[256] * 11, big, None) == code
+
+
+def test_bad_pointers_and_workspaces():
+    from paper_2407_02913_amd import binding
+
+    lib, d, big = binding.load(), _desc(), 1 << 40
+    at, f, b = C.addressof(d), C.c_size_t(), C.c_size_t()
+    assert lib.sfc_lowrank_sizes(at, C.byref(f), C.byref(b)) == 0 and f.value > 0 and b.value > 0
+    forward, backward = [at] + [256] * 8 + [big, None], [at] + [256] * 11 + [big, None]
+    for call, args, optional in ((lib.sfc_lowrank_add, forward, (5, 6)), (lib.sfc_lowrank_backward, backward, (6, 7))):
+        assert call(None, *args[1:]) == 1
+        space = len(args) - 3
+        for i in range(1, space):
+            assert call(*[None if k == i and i not in optional else 257 if k == i else v for k, v in enumerate(args)]) == 1, i
+        assert call(*[None if k == space else v for k, v in enumerate(args)]) == 6
+        assert call(*[264 if k == space else v for k, v in enumerate(args)]) == 1
+    assert lib.sfc_lowrank_add(*forward[:9], f.value - 1, None) == 6
+    assert lib.sfc_lowrank_backward(*backward[:12], b.value - 1, None) == 6
+    for name, code in (("base_stride", 1), ("y_stride", 1)):
+        assert lib.sfc_lowrank_add(C.addressof(_desc(**{name: 47})), *forward[1:]) == code
+    assert lib.sfc_lowrank_backward(C.addressof(_desc(dx_stride=63)), *backward[1:]) == 1
+    assert lib.sfc_lowrank_add(C.addressof(_desc(tokens=0)), *[None] * 8, 0, None) == 0
+
+
+@pytest.mark.gpu
+def test_bad_tensors():
+    from paper_2407_02913_amd import adapt, binding
+
+    d = make((20, 30, 40, 4, 2), torch.float32)
+    args = [d[n] for n in ("base", "x", "ids", "down", "up", "scale")]
+    adapt.add_adapters(*args)
+    for i, bad in ((0, d["base"][:, :7]), (0, d["base"].half()), (1, d["x"].cpu()), (1, d["x"].double()), (1, d["x"][0]),
+                   (2, d["ids"].long()), (2, d["ids"][:3]), (3, d["down"][:, :, :5]), (3, d["down"].half()),
+                   (4, d["up"][:1]), (4, d["up"].transpose(1, 2)), (5, d["scale"][:1]), (5, d["scale"].half())):
+        with pytest.raises(ValueError):
+            adapt.add_adapters(*[bad if k == i else v for k, v in enumerate(args)])
+    with pytest.raises(ValueError):
+        adapt.add_adapters(*args, out=d["base"].t().contiguous().t())
+    with pytest.raises(ValueError):
+        adapt.add_adapters_backward(d["dy"][:5], *args[1:])
+    wide = make((20, 30, 40, 130, 2), torch.float32)
+    with pytest.raises(binding.SfcError):
+        adapt.add_adapters(*[wide[n] for n in ("base", "x", "ids", "down", "up", "scale")])
