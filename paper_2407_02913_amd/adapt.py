@@ -24,11 +24,8 @@ _TYPE = {torch.float32: binding.TYPE_F32, torch.float16: binding.TYPE_F16, torch
          torch.int8: binding.TYPE_I8}
 
 
-def _require(ok, message):
-    if not ok:
-        raise ValueError(message)
-
-
+# (A small call is bound by what the host does for it: messages are made where a check fails, and a tensor's device is
+# compared by its number.)
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -47,6 +44,10 @@ def _call(device, name, *args):
 
 def _bytes(n, device):
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _misfit(name, want):
+    raise ValueError(f"{name}: {want}")
 
 
 # ---- group norm ----
@@ -74,7 +75,8 @@ class _Norm:
     """A checked description with its workspace sizes."""
 
     def __init__(self, shape, x, y, groups, eps, activation, y_scale):
-        _require(activation in binding.ACTIVATION, f"activation {activation!r}: one of {sorted(binding.ACTIVATION)}")
+        if activation not in binding.ACTIVATION:
+            raise ValueError(f"activation {activation!r}: one of {sorted(binding.ACTIVATION)}")
         self.desc = binding.GroupNormDesc(*shape, groups, x[0], y[0], x[1], y[1], binding.ACTIVATION[activation],
                                           eps, y_scale, x[2], x[3], y[2], y[3])
         self.at = C.addressof(self.desc)
@@ -95,30 +97,37 @@ def _norm(shape, x_stride, x_dtype, y_stride, y_dtype, groups, eps, activation, 
 
 
 def _check_norm(x, weight, bias):
-    _require(x.is_cuda and x.dim() == 4, f"x: a 4-axis tensor on the GPU, not {tuple(x.shape)} on {x.device}")
-    _require(x.dtype in _TYPE and x.dtype != torch.int8, f"x: float32, float16 or bfloat16, not {x.dtype}")
-    for name, p in (("weight", weight), ("bias", bias)):
-        if p is not None:
-            _require(p.dtype == torch.float32 and p.shape == x.shape[1:2] and p.device == x.device
-                     and (p.is_contiguous()), f"{name}: float32 [{x.shape[1]}] on {x.device}, contiguous")
+    if not x.is_cuda or x.dim() != 4 or x.dtype not in _TYPE or x.dtype is torch.int8:
+        _misfit("x", f"[N, C, H, W] in float32, float16 or bfloat16 on the GPU, not {tuple(x.shape)} {x.dtype} on {x.device}")
+    channels, device = x.shape[1], x.get_device()
+    for p in (weight, bias):
+        if p is not None and (p.dtype is not torch.float32 or p.dim() != 1 or p.shape[0] != channels
+                              or not p.is_contiguous() or p.get_device() != device):
+            _misfit("weight, bias", f"float32 [{channels}] on {x.device}, contiguous, not {tuple(p.shape)} {p.dtype} on {p.device}")
 
 
 def _norm_forward(x, groups, weight, bias, eps, activation, dtype, y_scale, channels_last):
+    """(y, the buffer that holds the statistics, [N, groups, 2], and the workspace behind them)"""
     _check_norm(x, weight, bias)
-    shape = tuple(x.shape)
-    if channels_last is None:
-        planes = (dtype == torch.int8 or x.is_contiguous()
-                  or _layout(shape, x.stride(), "x")[0] == binding.LAYOUT_NCHW)
+    shape, stride, device = tuple(x.shape), x.stride(), x.device
+    if channels_last is None and dtype is x.dtype and (
+            x.is_contiguous() or x.is_contiguous(memory_format=torch.channels_last)):
+        y = torch.empty_like(x)
     else:
-        planes = not channels_last
-    y = torch.empty(shape, dtype=dtype, device=x.device,
-                    memory_format=torch.contiguous_format if planes else torch.channels_last)
-    norm = _norm(shape, x.stride(), x.dtype, y.stride(), dtype, groups, eps, activation, y_scale)
-    stats = torch.empty((shape[0], groups, 2), dtype=torch.float32, device=x.device)
-    space = _bytes(norm.forward_bytes, x.device)
-    _call(x.device, "sfc_group_norm", norm.at, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(),
-          stats.data_ptr(), _ptr(space), norm.forward_bytes)
-    return y, stats
+        if channels_last is None:
+            planes = (dtype is torch.int8 or x.is_contiguous()
+                      or _layout(shape, stride, "x")[0] == binding.LAYOUT_NCHW)
+        else:
+            planes = not channels_last
+        y = torch.empty(shape, dtype=dtype, device=device,
+                        memory_format=torch.contiguous_format if planes else torch.channels_last)
+    norm = _norm(shape, stride, x.dtype, y.stride(), dtype, groups, eps, activation, y_scale)
+    first = (shape[0] * groups + 1) // 2 * 4  # floats, 16 bytes and more
+    buffer = torch.empty(first + norm.forward_bytes // 4, dtype=torch.float32, device=device)
+    at = buffer.data_ptr()
+    _call(device, "sfc_group_norm", norm.at, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), at,
+          at + 4 * first if norm.forward_bytes else None, norm.forward_bytes)
+    return y, buffer
 
 
 def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, activation="none", dtype=None,
@@ -130,7 +139,8 @@ def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, activation="
     weight and bias float32 [C] or None.  y has x's type and layout, or `dtype` (a 16-bit type from
     float32) and `channels_last`.  stats, float32 [N, groups, 2], are mean and 1 / sqrt(var + eps).
     activation: "none", "relu", "silu" or "gelu" (the exact one, with erf)."""
-    return _norm_forward(x, groups, weight, bias, eps, activation, dtype or x.dtype, 0.0, channels_last)
+    y, buffer = _norm_forward(x, groups, weight, bias, eps, activation, dtype or x.dtype, 0.0, channels_last)
+    return y, buffer.as_strided((x.shape[0], groups, 2), (2 * groups, 2, 1))
 
 
 def group_norm_i8(x, groups, weight=None, bias=None, eps=1e-5, activation="relu", *, y_scale):
@@ -143,11 +153,12 @@ def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, eps=1e-5, 
     """(dx, dweight, dbias) from y's gradient dy (x's type and layout), x and the forward call's stats.
     dweight and dbias, float32 [C], are sums over images in a fixed order."""
     _check_norm(x, weight, bias)
-    _require(dy.shape == x.shape and dy.dtype == x.dtype and dy.device == x.device,
-             f"dy: as x, {tuple(x.shape)} {x.dtype}, not {tuple(dy.shape)} {dy.dtype}")
-    _require(stats.shape == (x.shape[0], groups, 2) and stats.dtype == torch.float32 and stats.is_contiguous()
-             and stats.device == x.device, f"stats: float32 {(x.shape[0], groups, 2)}, as the forward call gave them")
     shape = tuple(x.shape)
+    if dy.shape != shape or dy.dtype is not x.dtype or dy.get_device() != x.get_device():
+        _misfit("dy", f"as x, {shape} {x.dtype} on {x.device}, not {tuple(dy.shape)} {dy.dtype} on {dy.device}")
+    if (stats.shape != (shape[0], groups, 2) or stats.dtype is not torch.float32 or not stats.is_contiguous()
+            or stats.get_device() != x.get_device()):
+        _misfit("stats", f"float32 {(shape[0], groups, 2)} on {x.device}, as the forward call gave them")
     norm = _norm(shape, x.stride(), x.dtype, dy.stride(), x.dtype, groups, eps, activation, 0.0)
     if x.is_contiguous() or x.is_contiguous(memory_format=torch.channels_last):
         dx = torch.empty_like(x)
@@ -183,7 +194,7 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none"):
     """y of group_norm_forward, in x's type and layout; differentiable in x, weight and bias."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
         return _GroupNorm.apply(x, weight, bias, groups, eps, activation)
-    return group_norm_forward(x, groups, weight, bias, eps, activation)[0]
+    return _norm_forward(x, groups, weight, bias, eps, activation, x.dtype, 0.0, None)[0]
 
 
 # ---- low-rank adapters ----
@@ -204,31 +215,44 @@ _lowrank = lru_cache(maxsize=1024)(_Lowrank)
 
 
 def _row_stride(t, what):
-    _require(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: a row's values lie side by side, not strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    rows, columns = t.shape
+    stride = t.stride()
+    if columns > 1 and stride[1] != 1:
+        _misfit(what, f"a row's values lie side by side, not strides {stride}")
+    return stride[0] if rows > 1 else 0
 
 
-def _check_adapters(x, ids, down, up, scale, outputs, wide):
-    """`outputs`, `wide`: (name, tensor or None) with as many columns as `up` has outputs, `down` inputs."""
-    _require(x.is_cuda and x.dim() == 2, f"x: [tokens, inputs] on the GPU, not {tuple(x.shape)} on {x.device}")
-    _require(x.dtype in _TYPE and x.dtype != torch.int8, f"x: float32, float16 or bfloat16, not {x.dtype}")
+def _dense(t, shape, dtype, device):
+    return t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == device
+
+
+def _check_adapters(x, ids, down, up, scale):
+    if not x.is_cuda or x.dim() != 2 or x.dtype not in _TYPE or x.dtype is torch.int8:
+        _misfit("x", f"[tokens, inputs] in float32, float16 or bfloat16 on the GPU, not {tuple(x.shape)} {x.dtype} on {x.device}")
     tokens, inputs = x.shape
-    _require(down.dim() == 3 and down.shape[2] == inputs and down.dtype == x.dtype and down.is_contiguous()
-             and down.device == x.device, f"down: {x.dtype} [adapters, rank, {inputs}] on {x.device}, contiguous")
+    dtype, device = x.dtype, x.get_device()
+    if down.dim() != 3 or up.dim() != 3:
+        _misfit("down, up", f"three axes each, not {tuple(down.shape)}, {tuple(up.shape)}")
     adapters, rank, _ = down.shape
-    _require(up.dim() == 3 and up.shape[0] == adapters and up.shape[2] == rank and up.dtype == x.dtype
-             and up.is_contiguous() and up.device == x.device,
-             f"up: {x.dtype} [{adapters}, outputs, {rank}] on {x.device}, contiguous")
-    _require(ids.shape == (tokens,) and ids.dtype == torch.int32 and ids.is_contiguous() and ids.device == x.device,
-             f"ids: int32 [{tokens}] on {x.device}, contiguous")
-    if scale is not None:
-        _require(scale.shape == (adapters,) and scale.dtype == torch.float32 and scale.is_contiguous()
-                 and scale.device == x.device, f"scale: float32 [{adapters}] on {x.device}, contiguous")
-    for columns, tensors in ((up.shape[1], outputs), (inputs, wide)):
-        for name, t in tensors:
-            _require(t is None or (t.shape == (tokens, columns) and t.dtype == x.dtype and t.device == x.device),
-                     f"{name}: {x.dtype} [{tokens}, {columns}] on {x.device}")
-    return tokens, inputs, up.shape[1], rank, adapters, _TYPE[x.dtype]
+    outputs = up.shape[1]
+    if not _dense(down, (adapters, rank, inputs), dtype, device):
+        _misfit("down", f"{dtype} [adapters, rank, {inputs}] on {x.device}, contiguous, not {tuple(down.shape)} {down.dtype}")
+    if not _dense(up, (adapters, outputs, rank), dtype, device):
+        _misfit("up", f"{dtype} [{adapters}, outputs, {rank}] on {x.device}, contiguous, not {tuple(up.shape)} {up.dtype}")
+    if not _dense(ids, (tokens,), torch.int32, device):
+        _misfit("ids", f"int32 [{tokens}] on {x.device}, contiguous, not {tuple(ids.shape)} {ids.dtype}")
+    if scale is not None and not _dense(scale, (adapters,), torch.float32, device):
+        _misfit("scale", f"float32 [{adapters}] on {x.device}, contiguous, not {tuple(scale.shape)} {scale.dtype}")
+    return tokens, inputs, outputs, rank, adapters, _TYPE[dtype]
+
+
+def _check_rows(name, t, x, columns):
+    """Row stride of a [tokens, columns] tensor of x's type, 0 where there is none."""
+    if t is None:
+        return 0
+    if t.shape != (x.shape[0], columns) or t.dtype is not x.dtype or t.get_device() != x.get_device():
+        _misfit(name, f"{x.dtype} [{x.shape[0]}, {columns}] on {x.device}, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    return _row_stride(t, name)
 
 
 def add_adapters(base, x, ids, down, up, scale=None, out=None):
@@ -238,11 +262,13 @@ def add_adapters(base, x, ids, down, up, scale=None, out=None):
     x [tokens, inputs]; base [tokens, outputs], the shared projection's output, or None; down [adapters, rank, inputs] and
     up [adapters, outputs, rank]; one type, float32, float16 or bfloat16.  ids, int32 [tokens]: any order; an id
     outside the adapters is none, y = base.  scale, float32 [adapters], or None.  `out` may be base."""
-    fields = _check_adapters(x, ids, down, up, scale, (("base", base), ("out", out)), ())
-    y = torch.empty((fields[0], fields[2]), dtype=x.dtype, device=x.device) if out is None else out
-    plan = _lowrank(*fields, _row_stride(x, "x"), 0 if base is None else _row_stride(base, "base"), _row_stride(y, "out"), 0)
-    space = _bytes(plan.forward_bytes, x.device)
-    _call(x.device, "sfc_lowrank_add", plan.at, x.data_ptr(), ids.data_ptr(), down.data_ptr(), up.data_ptr(), _ptr(scale),
+    fields = _check_adapters(x, ids, down, up, scale)
+    outputs, device = fields[2], x.device
+    plan = _lowrank(*fields, _row_stride(x, "x"), _check_rows("base", base, x, outputs),
+                    _check_rows("out", out, x, outputs), 0)
+    y = torch.empty((fields[0], outputs), dtype=x.dtype, device=device) if out is None else out
+    space = _bytes(plan.forward_bytes, device)
+    _call(device, "sfc_lowrank_add", plan.at, x.data_ptr(), ids.data_ptr(), down.data_ptr(), up.data_ptr(), _ptr(scale),
           _ptr(base), y.data_ptr(), _ptr(space), plan.forward_bytes)
     return y
 
@@ -250,11 +276,11 @@ def add_adapters(base, x, ids, down, up, scale=None, out=None):
 def add_adapters_backward(dy, x, ids, down, up, scale=None, dx_base=None):
     """(dx, d_down, d_up) from y's gradient dy: dx = dx_base + scale[l] (up[l] down[l])^T dy, where dx_base is the shared
     projection's part or None; the factors' gradients, in their type, are sums over each adapter's tokens."""
-    fields = _check_adapters(x, ids, down, up, scale, (("dy", dy),), (("dx_base", dx_base),))
+    fields = _check_adapters(x, ids, down, up, scale)
+    plan = _lowrank(*fields, _row_stride(x, "x"), _check_rows("dx_base", dx_base, x, fields[1]),
+                    _check_rows("dy", dy, x, fields[2]), 0)
     dx = torch.empty((fields[0], fields[1]), dtype=x.dtype, device=x.device)
     d_down, d_up = torch.empty_like(down), torch.empty_like(up)
-    plan = _lowrank(*fields, _row_stride(x, "x"), 0 if dx_base is None else _row_stride(dx_base, "dx_base"),
-                    _row_stride(dy, "dy"), 0)
     space = _bytes(plan.backward_bytes, x.device)
     _call(x.device, "sfc_lowrank_backward", plan.at, x.data_ptr(), dy.data_ptr(), ids.data_ptr(), down.data_ptr(),
           up.data_ptr(), _ptr(scale), _ptr(dx_base), dx.data_ptr(), d_down.data_ptr(), d_up.data_ptr(), _ptr(space),
@@ -293,22 +319,24 @@ def _distill(rows, classes, top, dtype, wide, tail, temperature, logits_stride, 
 
 
 def _check_distill(logits, values, index, row_scale, temperature, tail, grad=None):
-    _require(logits.is_cuda and logits.dim() == 2 and logits.shape[1] > 0,
-             f"logits: [rows, classes] on the GPU, not {tuple(logits.shape)} on {logits.device}")
-    _require(logits.dtype in _TYPE and logits.dtype != torch.int8,
-             f"logits: float32, float16 or bfloat16, not {logits.dtype}")
+    if (not logits.is_cuda or logits.dim() != 2 or logits.shape[1] == 0 or logits.dtype not in _TYPE
+            or logits.dtype is torch.int8):
+        _misfit("logits", f"[rows, classes] in float32, float16 or bfloat16 on the GPU, not {tuple(logits.shape)} "
+                f"{logits.dtype} on {logits.device}")
     rows, classes = logits.shape
-    _require(values.dim() == 2 and values.shape[0] == rows and values.dtype == torch.float32
-             and values.device == logits.device, f"values: float32 [{rows}, top] on {logits.device}")
-    _require(index.shape == values.shape and index.dtype in (torch.int32, torch.int64) and index.device == logits.device,
-             f"index: int32 or int64 {tuple(values.shape)} on {logits.device}")
-    if row_scale is not None:
-        _require(row_scale.shape == (rows,) and row_scale.dtype == torch.float32 and row_scale.is_contiguous()
-                 and row_scale.device == logits.device, f"row_scale: float32 [{rows}] on {logits.device}, contiguous")
-    desc = _distill(rows, classes, values.shape[1], logits.dtype, index.dtype == torch.int64, tail, temperature,
-                    _row_stride(logits, "logits"), 0 if grad is None else _row_stride(grad, "grad"),
-                    _row_stride(values, "values"), _row_stride(index, "index"))
-    return C.addressof(desc)
+    device = logits.get_device()
+    if values.dim() != 2 or values.shape[0] != rows or values.dtype is not torch.float32 or values.get_device() != device:
+        _misfit("values", f"float32 [{rows}, top] on {logits.device}, not {tuple(values.shape)} {values.dtype}")
+    wide = index.dtype is torch.int64
+    if (index.shape != values.shape or not (wide or index.dtype is torch.int32) or index.get_device() != device):
+        _misfit("index", f"int32 or int64 {tuple(values.shape)} on {logits.device}, not {tuple(index.shape)} {index.dtype}")
+    if row_scale is not None and not _dense(row_scale, (rows,), torch.float32, device):
+        _misfit("row_scale", f"float32 [{rows}] on {logits.device}, contiguous")
+    if grad is not None and (grad.shape != logits.shape or grad.dtype is not logits.dtype or grad.get_device() != device):
+        _misfit("out", f"as the logits, {tuple(logits.shape)} {logits.dtype}, not {tuple(grad.shape)} {grad.dtype}")
+    return _distill(rows, classes, values.shape[1], logits.dtype, wide, tail, temperature, _row_stride(logits, "logits"),
+                    0 if grad is None else _row_stride(grad, "out"), _row_stride(values, "values"),
+                    _row_stride(index, "index"))
 
 
 def distill_loss(logits, values, index, row_scale=None, temperature=1.0, tail=False):
@@ -319,10 +347,10 @@ def distill_loss(logits, values, index, row_scale=None, temperature=1.0, tail=Fa
     their softmax at the temperature.  tail: the values are log-probabilities at the temperature instead, and what
     they leave is one more outcome, against the student's mass outside the places.  A place outside the classes
     is padding.  row_scale, float32 [rows]: rows of 0 are masked (loss 0, not read)."""
-    at = _check_distill(logits, values, index, row_scale, temperature, tail)
+    desc = _check_distill(logits, values, index, row_scale, temperature, tail)
     loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
     stats = torch.empty((logits.shape[0], 4), dtype=torch.float32, device=logits.device)
-    _call(logits.device, "sfc_distill_loss", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
+    _call(logits.device, "sfc_distill_loss", C.addressof(desc), logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
           loss.data_ptr(), stats.data_ptr())
     return loss, stats
 
@@ -330,13 +358,11 @@ def distill_loss(logits, values, index, row_scale=None, temperature=1.0, tail=Fa
 def distill_grad(logits, values, index, stats, row_scale=None, temperature=1.0, tail=False, out=None):
     """The gradient of sum(row_scale loss) in the logits, in their type, from distill_loss's stats.  `out` may be
     the logits themselves."""
-    grad = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
-    _require(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device,
-             f"out: as the logits, {tuple(logits.shape)} {logits.dtype}")
-    _require(stats.shape == (logits.shape[0], 4) and stats.dtype == torch.float32 and stats.is_contiguous()
-             and stats.device == logits.device, f"stats: float32 [{logits.shape[0]}, 4], as distill_loss gave them")
-    at = _check_distill(logits, values, index, row_scale, temperature, tail, grad)
-    _call(logits.device, "sfc_distill_grad", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
+    desc = _check_distill(logits, values, index, row_scale, temperature, tail, out)
+    if not _dense(stats, (logits.shape[0], 4), torch.float32, logits.get_device()):
+        _misfit("stats", f"float32 [{logits.shape[0]}, 4] on {logits.device}, as distill_loss gave them")
+    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if out is None else out
+    _call(logits.device, "sfc_distill_grad", C.addressof(desc), logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
           stats.data_ptr(), grad.data_ptr())
     return grad
 
@@ -344,12 +370,10 @@ def distill_grad(logits, values, index, stats, row_scale=None, temperature=1.0, 
 def distill_loss_and_grad(logits, values, index, row_scale=None, temperature=1.0, tail=False, out=None):
     """(loss, gradient) as of distill_loss and distill_grad, the logits read once: for a training step whose loss
     is sum(row_scale loss)."""
-    grad = torch.empty_like(logits, memory_format=torch.contiguous_format) if out is None else out
-    _require(grad.shape == logits.shape and grad.dtype == logits.dtype and grad.device == logits.device,
-             f"out: as the logits, {tuple(logits.shape)} {logits.dtype}")
-    at = _check_distill(logits, values, index, row_scale, temperature, tail, grad)
+    desc = _check_distill(logits, values, index, row_scale, temperature, tail, out)
+    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if out is None else out
     loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
-    _call(logits.device, "sfc_distill_loss_grad", at, logits.data_ptr(), values.data_ptr(), index.data_ptr(),
+    _call(logits.device, "sfc_distill_loss_grad", C.addressof(desc), logits.data_ptr(), values.data_ptr(), index.data_ptr(),
           _ptr(row_scale), loss.data_ptr(), grad.data_ptr())
     return loss, grad
 

@@ -18,12 +18,13 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A wave or a workgroup that owns a row.
-template <bool WAVE>
+// A wave (LANES = 64) or a workgroup that owns a row.
+template <int LANES>
 struct Team {
+  static constexpr bool WAVE = LANES == 64;
   float* scratch;  // 16 floats a use
   __device__ __forceinline__ int lane() const { return WAVE ? threadIdx.x & 63 : threadIdx.x; }
-  __device__ __forceinline__ int size() const { return WAVE ? 64 : blockDim.x; }
+  __device__ __forceinline__ int size() const { return LANES; }
   __device__ __forceinline__ void sync() const {
     if constexpr (WAVE) {
       // lanes of one wave: LDS accesses stay in order once the compiler keeps them so
@@ -42,7 +43,7 @@ struct Team {
       if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
       __syncthreads();
       v = 0.0f;
-      for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v += at[i];
+      for (int i = 0; i < LANES / 64; ++i) v += at[i];
     }
     return v;
   }
@@ -53,26 +54,27 @@ struct Team {
       scratch += 16;
       if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
       __syncthreads();
-      for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v = fmaxf(v, at[i]);
+      for (int i = 0; i < LANES / 64; ++i) v = fmaxf(v, at[i]);
     }
     return v;
   }
 };
 constexpr int kUses = 8;  // sums and maxima of a row
 
-// LDS of a row: scratch; of each of the teacher's places its probability, that of all entries for the same place,
-// its logit and where it is; a byte for each vector (tail).
+// LDS of a row: scratch; of each of the teacher's entries its probability, that of all entries for the same place, the
+// student's logit, the teacher's value and the place; a byte for each vector (tail).
 struct RowSpace {
   float* scratch;
   float* p;
   float* all;
   float* logit;
+  float* value;
   int* at;
   unsigned* map;
 };
 
 int row_space_bytes(int top, int items, bool tail) {
-  return kUses * 16 * 4 + (top + 3) / 4 * 4 * 16 + (tail ? (items + 15) / 16 * 16 : 0);
+  return kUses * 16 * 4 + (top + 3) / 4 * 4 * 20 + (tail ? (items + 15) / 16 * 16 : 0);
 }
 
 __device__ __forceinline__ RowSpace row_space(char* base, int top) {
@@ -82,7 +84,8 @@ __device__ __forceinline__ RowSpace row_space(char* base, int top) {
   s.p = s.scratch + kUses * 16;
   s.all = s.p + places;
   s.logit = s.all + places;
-  s.at = reinterpret_cast<int*>(s.logit + places);
+  s.value = s.logit + places;
+  s.at = reinterpret_cast<int*>(s.value + places);
   s.map = reinterpret_cast<unsigned*>(s.at + places);
   return s;
 }
@@ -98,31 +101,49 @@ struct Row {
   float mass;             // sum of the teacher's probabilities, the rest included
 };
 
+// One of a row's entries: place (-1: none), value, and the student's logit there.
+struct Entry {
+  int place;
+  float value, logit;
+};
+
+__device__ __forceinline__ Entry load_entry(const DistillArgs& a, int64_t row, int k) {
+  Entry e = {-1, 0.0f, 0.0f};
+  if (k < a.top) {
+    const int64_t at = a.wide ? static_cast<const int64_t*>(a.index)[row * a.index_stride + k]
+                              : static_cast<const int32_t*>(a.index)[row * a.index_stride + k];
+    e.place = at >= 0 && at < a.classes ? (int)at : -1;
+    e.value = a.values[row * a.values_stride + k];
+  }
+  return e;
+}
+
 // The teacher's entries into LDS (a place outside the classes is none) and, with a tail, the map of vectors that hold
-// any.  Returns (sum of p, log of what the exponentials were divided by); ends with a barrier, before which every
-// logit at a place has been read.
-template <typename T, bool WAVE>
-__device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t row, const RowSpace& s, Team<WAVE>& team,
-                                                const T* logits) {
+// any; `own` is the lane's first entry, loaded before.  Returns (sum of p, log of what the exponentials were divided by);
+// ends with a barrier, before which every logit at a place has been read.
+template <typename T, int LANES>
+__device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t row, const RowSpace& s, Team<LANES>& team,
+                                                const T* logits, Entry own) {
   constexpr int V = kVec<T>;
   const int lane = team.lane(), size = team.size();
-  const float* values = a.values + row * a.values_stride;
   if (a.tail) {
     const int words = (a.classes + 4 * V - 1) / (4 * V);
     for (int i = lane; i < words; i += size) s.map[i] = 0u;
     team.sync();
   }
   float top = -INFINITY;
+#pragma unroll 1
   for (int k = lane; k < a.top; k += size) {
-    const int64_t at = a.wide ? static_cast<const int64_t*>(a.index)[row * a.index_stride + k]
-                              : static_cast<const int32_t*>(a.index)[row * a.index_stride + k];
-    const int place = at >= 0 && at < a.classes ? (int)at : -1;
-    const float v = values[k];
+    if (k != lane) {
+      own = load_entry(a, row, k);
+      if (own.place >= 0) own.logit = (float)logits[own.place];
+    }
+    const int place = own.place;
     s.at[k] = place;
-    s.p[k] = v;
+    s.p[k] = s.value[k] = own.value;
     if (place >= 0) {
-      s.logit[k] = (float)logits[place];
-      top = fmaxf(top, v);
+      s.logit[k] = own.logit;
+      top = fmaxf(top, own.value);
       if (a.tail) atomicOr(&s.map[place / (4 * V)], 1u << (place / V % 4 * 8 + place % V));
     }
   }
@@ -132,6 +153,7 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
     about = top == -INFINITY ? 0.0f : top;
     c = 1.0f / a.temperature;
     float sum = 0.0f;
+#pragma unroll 1
     for (int k = lane; k < a.top; k += size)
       if (s.at[k] >= 0) sum += __expf((s.p[k] - about) * c);
     sum = team.sum(sum);
@@ -139,6 +161,7 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
     log_sum = about * c + __logf(sum);
   }
   float mass = 0.0f;
+#pragma unroll 1
   for (int k = lane; k < a.top; k += size) {
     const float p = s.at[k] < 0 ? 0.0f : __expf((s.p[k] - about) * c) * scale;
     s.p[k] = p;
@@ -148,9 +171,11 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
   team.sync();
   if (a.grad) {
     // entries for one place, added in their order by each of them
-    for (int k = lane; k < a.top; k += size) {
+  #pragma unroll 1
+  for (int k = lane; k < a.top; k += size) {
       const int mine = s.at[k];
       float all = 0.0f;
+#pragma unroll 4
       for (int i = 0; i < a.top; ++i) all += s.at[i] == mine ? s.p[i] : 0.0f;
       s.all[k] = all;
     }
@@ -159,37 +184,41 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
   return make_float2(mass, log_sum);
 }
 
+// exp((s - max) / T) with c = log2 e / T and top = max c rounded: what that rounding is worth multiplies all of a row's
+// exponentials alike and leaves their ratios.
+__device__ __forceinline__ float scaled_exp(float s, float c, float top) {
+  return __builtin_amdgcn_exp2f(fmaf(s, c, -top));
+}
+
 // The elements of this lane's vector that are the teacher's.
 __device__ __forceinline__ unsigned top_elements(const RowSpace& s, int item) {
   return s.map[item >> 2] >> (item & 3) * 8 & 255u;
 }
 
-// The gradient of a vector outside the teacher's places, stored.
+// The gradient of a vector outside the teacher's places.
 template <typename T>
-__device__ __forceinline__ void store_grad(const DistillArgs& a, const Row& row, float scale, int item, const raw4& raw,
-                                           T* grad) {
-  constexpr int V = kVec<T>;
+__device__ __forceinline__ void gradient(const DistillArgs& a, const Row& row, float scale, const raw4& raw,
+                                         float (&v)[kVec<T>]) {
   const float c = kLog2e / a.temperature, unit = scale / row.sum * (row.mass - row.ratio);
-  float v[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) v[j] = __builtin_amdgcn_exp2f((element<T>(raw, j) - row.max) * c) * unit;
-  store_vec<T, V>(grad + (int64_t)item * V, v, min(V, a.classes - item * V));
+  for (int j = 0; j < kVec<T>; ++j) v[j] = scaled_exp(element<T>(raw, j), c, row.max * c) * unit;
 }
 
 // The gradient at the teacher's places, by the wave whose lanes stored their vectors: a wave's stores to one address
 // stay in order.
-template <typename T, bool WAVE>
-__device__ __forceinline__ void store_places(const DistillArgs& a, const RowSpace& s, Team<WAVE>& team, const Row& row,
+template <typename T, int LANES>
+__device__ __forceinline__ void store_places(const DistillArgs& a, const RowSpace& s, Team<LANES>& team, const Row& row,
                                              float scale, T* grad) {
   constexpr int V = kVec<T>;
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   const float c = kLog2e / a.temperature;
+#pragma unroll 1
   for (int k = threadIdx.x & 63; k < a.top; k += 64) {
     const int place = s.at[k];
-    if (place < 0 || (!WAVE && place / V % team.size() / 64 != (int)(threadIdx.x >> 6))) continue;
-    const float q = __builtin_amdgcn_exp2f((s.logit[k] - row.max) * c) / row.sum;
+    if (place < 0 || (LANES > 64 && place / V % LANES / 64 != (int)(threadIdx.x >> 6))) continue;
+    const float q = scaled_exp(s.logit[k], c, row.max * c) / row.sum;
     grad[place] = (T)((q * row.mass - s.all[k]) * scale);
   }
 }
@@ -212,24 +241,25 @@ __device__ __forceinline__ void add_exp(const DistillArgs& a, const RowSpace& s,
   const float c = kLog2e / a.temperature;
   float e[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) e[j] = __builtin_amdgcn_exp2f((element<T>(raw, j) - max) * c);
+  for (int j = 0; j < V; ++j) e[j] = scaled_exp(element<T>(raw, j), c, max * c);
   if (a.tail) {
     const unsigned mask = live ? top_elements(s, item) : 0u;
+    if (mask) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const bool in = mask >> j & 1u;
-      *rest += in ? 0.0f : e[j];
-      *top += in ? e[j] : 0.0f;
+      for (int j = 0; j < V; ++j) {
+        const bool in = mask >> j & 1u;
+        *top += in ? e[j] : 0.0f;
+        e[j] = in ? 0.0f : e[j];
+      }
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j) *rest += e[j];
   }
+#pragma unroll
+  for (int j = 0; j < V; ++j) *rest += e[j];
 }
 
 // Loss and statistics once the student's sums stand.
-template <bool WAVE>
-__device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, const RowSpace& s, Team<WAVE>& team,
+template <int LANES>
+__device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, const RowSpace& s, Team<LANES>& team,
                                            float2 teacher, float max, float rest, float top) {
   const float c = 1.0f / a.temperature;
   Row r;
@@ -238,14 +268,14 @@ __device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, co
   r.ratio = 0.0f;
   r.mass = teacher.x;
   const float log_sum = __logf(r.sum);
-  const float* values = a.values + row * a.values_stride;
   float loss = 0.0f;
+#pragma unroll 1
   for (int k = team.lane(); k < a.top; k += team.size()) {
     const int place = s.at[k];
     const float p = s.p[k];
     if (place >= 0 && p != 0.0f) {
       const float log_q = (s.logit[k] - max) * c - log_sum;
-      const float log_p = a.tail ? values[k] : values[k] * c - teacher.y;
+      const float log_p = a.tail ? s.value[k] : s.value[k] * c - teacher.y;
       loss += p * (log_p - log_q);
     }
   }
@@ -268,14 +298,15 @@ __device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, co
 }
 
 // A row whose scale is zero: nothing of it is read.
-template <typename T, bool WAVE>
-__device__ __forceinline__ void masked_row(const DistillArgs& a, int64_t row, Team<WAVE>& team) {
+template <typename T, int LANES>
+__device__ __forceinline__ void masked_row(const DistillArgs& a, int64_t row, Team<LANES>& team) {
   if (a.loss && team.lane() == 0) {
     a.loss[row] = 0.0f;
     if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(0.0f, 1.0f, 0.0f, 0.0f);
   }
   if (a.grad) {
     T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
+#pragma unroll 1
     for (int q = team.lane(); q * kVec<T> < a.classes; q += team.size()) store_nothing<T>(a, q, grad);
   }
 }
@@ -287,62 +318,142 @@ __device__ __forceinline__ Row row_of_stats(const DistillArgs& a, int64_t row) {
   return r;
 }
 
-// A row to a team, NV vectors to a lane.
-template <typename T, int NV, bool WAVE>
-__global__ __launch_bounds__(WAVE ? 256 : 1024) void distill_rows(DistillArgs a, int space) {
+// A value that is the same in all lanes, for the compiler.
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
+// The largest element of NV vectors.  16-bit types: two at a time as integers, which order like the floats where the
+// largest is not negative (and a negative result tells that it was).
+template <typename T, int NV>
+__device__ __forceinline__ float largest(raw4 (&raw)[NV]) {
   constexpr int V = kVec<T>;
-  extern __shared__ float4 lds[];
-  const int64_t row = WAVE ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (WAVE && row >= a.rows) return;
-  const RowSpace s = row_space(reinterpret_cast<char*>(lds) + (WAVE ? (threadIdx.x >> 6) * space : 0), a.top);
-  Team<WAVE> team{s.scratch};
-  const float scale = a.row_scale ? a.row_scale[row] : 1.0f;
-  if (scale == 0.0f) {
-    masked_row<T, WAVE>(a, row, team);
-    return;
+  if constexpr (sizeof(T) == 2) {
+    typedef short s2 __attribute__((ext_vector_type(2)));
+    s2 m = {-32768, -32768};
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const unsigned two = raw[u][d];  // (a copy: a bit cast of the vector's element itself takes the first one)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(s2, two));
+      }
+    const short top = m[0] > m[1] ? m[0] : m[1];
+    if (top >= 0) return (float)__builtin_bit_cast(T, top);
   }
-  const T* logits = static_cast<const T*>(a.logits) + row * a.logits_stride;
-  const int64_t room = (a.rows - 1 - row) * a.logits_stride + a.classes;
-  const int items = (a.classes + V - 1) / V, lane = team.lane(), size = team.size();
-  raw4 raw[NV];
+  float max = -INFINITY;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
-    const int q = lane + u * size;
-    raw[u] = raw4{kNone<T>, kNone<T>, kNone<T>, kNone<T>};
-    if (q < items) raw[u] = load_cut(logits + (int64_t)q * V, a.classes - q * V, room - (int64_t)q * V, kNone<T>);
+#pragma unroll
+    for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(raw[u], j));
+    asm volatile("" : "+v"(raw[u]));  // (the loaded bits are kept, not the floats made of them)
   }
-  const float2 teacher = stage_teacher<T, WAVE>(a, row, s, team, logits);
-  Row r;
-  if (a.loss) {
-    float max = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(raw[u], j));
-      asm volatile("" : "+v"(raw[u]));  // (the loaded bits are kept, not the floats made of them)
+  return max;
+}
+
+// A row to a team, NV vectors to a lane.  A team takes every gridDim.x-th row, and loads a vector of its next one as soon
+// as the gradient of that vector has left: reading runs beside the exponentials and the writing.  Addresses are a
+// scalar for the team and a lane's offset, so that the registers are the row's; the vector that the row's end cuts, if
+// any, is loaded and stored by itself.
+template <typename T, int NV, int LANES, bool LOSS, bool GRAD>
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? 4 : NV == 8 ? 5 : 2) void distill_rows(DistillArgs a, int space) {
+  constexpr int V = kVec<T>;
+  constexpr int TEAMS = LANES == 64 ? 4 : 1;
+  extern __shared__ float4 lds[];
+  const int mine = LANES == 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0;
+  const int64_t first = (int64_t)blockIdx.x * TEAMS + mine, rows_step = (int64_t)gridDim.x * TEAMS;
+  const RowSpace s = row_space(reinterpret_cast<char*>(lds) + mine * space, a.top);
+  Team<LANES> team{s.scratch};
+  const int lane = team.lane(), rest_elements = a.classes % V, whole = a.classes / V;
+  // Vectors u < full are whole for every lane, of vector `full` the first `ragged` lanes' are; the element count's rest
+  // lies behind them, with one lane.
+  const int full = whole / LANES, ragged = whole - full * LANES;
+  const bool cuts = rest_elements != 0 && lane == ragged;
+  const unsigned offset = (unsigned)lane * V;
+  constexpr raw4 none = {kNone<T>, kNone<T>, kNone<T>, kNone<T>};
+  auto load = [&](const T* at, int u) {
+    raw4 r = none;
+    if (u < full) r = load16(at + u * LANES * V + offset);
+    else if (u == full && lane < ragged) r = load16(at + u * LANES * V + offset);
+    return r;
+  };
+  auto load_the_cut = [&](int64_t row, const T* at) {
+    return cuts ? load_cut(at + whole * V, rest_elements, (a.rows - 1 - row) * a.logits_stride + rest_elements, kNone<T>)
+                : none;
+  };
+  auto row_at = [&](int64_t row) { return static_cast<const T*>(a.logits) + row * a.logits_stride; };
+  // The first row from `row` on that is not masked; masked ones on the way are done with.
+  float scale = 1.0f;
+  auto unmasked = [&](int64_t row) {
+    while (row < a.rows && a.row_scale && (scale = uniform(a.row_scale[row])) == 0.0f) {
+      masked_row<T, LANES>(a, row, team);
+      row += rows_step;
     }
-    max = team.max(max);
-    float rest = 0.0f, top = 0.0f;
+    return row;
+  };
+  raw4 raw[NV], cut;
+  int64_t row = unmasked(first);
+  if (row >= a.rows) return;
+  // (a row's entries are asked for ahead of its logits, which would keep them waiting)
+  Entry entry = load_entry(a, row, lane);
+  {
+    const T* at = row_at(row);
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const int q = lane + u * size;
-      add_exp<T>(a, s, raw[u], q, q < items, max, &rest, &top);
-      asm volatile("" : "+v"(raw[u]));
-    }
-    rest = team.sum(rest);
-    if (a.tail) top = team.sum(top);
-    r = finish_loss<WAVE>(a, row, s, team, teacher, max, rest, a.tail ? top : 0.0f);
-  } else {
-    r = row_of_stats(a, row);
+    for (int u = 0; u < NV; ++u) raw[u] = load(at, u);
+    cut = load_the_cut(row, at);
+    if (entry.place >= 0) entry.logit = (float)at[entry.place];
   }
-  if (a.grad) {
-    T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
+  for (;;) {
+    const float unit = scale * a.temperature;
+    const int64_t next = unmasked(row + rows_step);
+    // (behind the last row: that row once more, for nothing, so that the loads have no condition)
+    const int64_t then = next < a.rows ? next : row;
+    const T* next_at = row_at(then);
+    team.scratch = s.scratch;
+    const float2 teacher = stage_teacher<T, LANES>(a, row, s, team, row_at(row), entry);
+    entry = load_entry(a, then, lane);
+    Row r;
+    if constexpr (LOSS) {
+      float max = largest<T, NV>(raw);
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const int q = lane + u * size;
-      if (q < items) store_grad<T>(a, r, scale * a.temperature, q, raw[u], grad);
+      for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(cut, j));
+      max = team.max(max);
+      float rest = 0.0f, top = 0.0f;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (u <= full) add_exp<T>(a, s, raw[u], lane + u * LANES, u < full || lane < ragged, max, &rest, &top);
+        asm volatile("" : "+v"(raw[u]));
+      }
+      if (rest_elements) add_exp<T>(a, s, cut, whole, cuts, max, &rest, &top);
+      rest = team.sum(rest);
+      if (a.tail) top = team.sum(top);
+      r = finish_loss<LANES>(a, row, s, team, teacher, max, rest, a.tail ? top : 0.0f);
+    } else {
+      r = row_of_stats(a, row);
     }
-    store_places<T, WAVE>(a, s, team, r, scale * a.temperature, grad);
+    if (entry.place >= 0) entry.logit = (float)next_at[entry.place];
+    if constexpr (GRAD) {
+      T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
+      float v[V];
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        if (u <= full) {
+          gradient<T>(a, r, unit, raw[u], v);
+          if (u < full || lane < ragged) store_vec<T, V>(grad + u * LANES * V + offset, v, V);
+          raw[u] = load(next_at, u);
+        }
+      }
+      gradient<T>(a, r, unit, cut, v);
+      if (cuts) store_vec<T, V>(grad + whole * V, v, rest_elements);
+      store_places<T, LANES>(a, s, team, r, unit, grad);
+    } else {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) raw[u] = load(next_at, u);
+    }
+    cut = load_the_cut(then, next_at);
+    if (next >= a.rows) return;
+    row = next;
+    team.sync();  // (the next row's teacher takes this one's place)
   }
 }
 
@@ -353,20 +464,22 @@ __global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
   extern __shared__ float4 lds[];
   const int64_t row = blockIdx.x;
   const RowSpace s = row_space(reinterpret_cast<char*>(lds), a.top);
-  Team<false> team{s.scratch};
+  Team<1024> team{s.scratch};
   const float scale = a.row_scale ? a.row_scale[row] : 1.0f;
   if (scale == 0.0f) {
-    masked_row<T, false>(a, row, team);
+    masked_row<T, 1024>(a, row, team);
     return;
   }
   const T* logits = static_cast<const T*>(a.logits) + row * a.logits_stride;
   const int64_t room = (a.rows - 1 - row) * a.logits_stride + a.classes;
-  const int items = (a.classes + V - 1) / V, lane = threadIdx.x, size = blockDim.x;
+  const int items = (a.classes + V - 1) / V, lane = threadIdx.x, size = 1024;
   auto load = [&](int q) {
     if (q >= items) return raw4{kNone<T>, kNone<T>, kNone<T>, kNone<T>};
     return load_cut(logits + (int64_t)q * V, a.classes - q * V, room - (int64_t)q * V, kNone<T>);
   };
-  const float2 teacher = stage_teacher<T, false>(a, row, s, team, logits);
+  Entry entry = load_entry(a, row, lane);
+  if (entry.place >= 0) entry.logit = (float)logits[entry.place];
+  const float2 teacher = stage_teacher<T, 1024>(a, row, s, team, logits, entry);
   Row r;
   if (a.loss) {
     // each thread its own running maximum, its sums scaled down when that grows
@@ -398,7 +511,7 @@ __global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
     rest = team.sum(rest * f);
     top = a.tail ? team.sum(top * f) : 0.0f;
     if (m == -INFINITY) rest = NAN;
-    r = finish_loss<false>(a, row, s, team, teacher, m, rest, top);
+    r = finish_loss<1024>(a, row, s, team, teacher, m, rest, top);
   } else {
     r = row_of_stats(a, row);
   }
@@ -411,32 +524,39 @@ __global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int q = q0 + u * size + lane;
-        if (q < items) store_grad<T>(a, r, scale * a.temperature, q, raw[u], grad);
+        float v[V];
+        gradient<T>(a, r, scale * a.temperature, raw[u], v);
+        if (q < items) store_vec<T, V>(grad + (int64_t)q * V, v, min(V, a.classes - q * V));
       }
     }
-    store_places<T, false>(a, s, team, r, scale * a.temperature, grad);
+    store_places<T, 1024>(a, s, team, r, scale * a.temperature, grad);
   }
 }
 
-template <typename T, int NV, bool WAVE>
-hipError_t run_rows(const DistillArgs& a, int threads, int items, hipStream_t s) {
+template <typename T, int NV, int LANES>
+hipError_t run_rows(const DistillArgs& a, int items, int per_unit, hipStream_t s) {
+  constexpr int TEAMS = LANES == 64 ? 4 : 1;
   const int space = row_space_bytes(a.top, items, a.tail);
-  const unsigned blocks = WAVE ? (unsigned)((a.rows + 3) / 4) : (unsigned)a.rows;
-  distill_rows<T, NV, WAVE><<<dim3(blocks), dim3((unsigned)threads), WAVE ? 4 * space : space, s>>>(a, space);
+  const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS, most = 256 * (int64_t)per_unit;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(LANES == 64 ? 256 : LANES);
+  if (a.loss && a.grad) distill_rows<T, NV, LANES, true, true><<<grid, block, TEAMS * space, s>>>(a, space);
+  else if (a.loss) distill_rows<T, NV, LANES, true, false><<<grid, block, TEAMS * space, s>>>(a, space);
+  else distill_rows<T, NV, LANES, false, true><<<grid, block, TEAMS * space, s>>>(a, space);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t run_distill(const DistillArgs& a, hipStream_t s) {
   const int items = (a.classes + kVec<T> - 1) / kVec<T>;
-  if (items <= 64) return run_rows<T, 1, true>(a, 256, items, s);
-  if (items <= 128) return run_rows<T, 2, true>(a, 256, items, s);
-  if (items <= 256) return run_rows<T, 4, true>(a, 256, items, s);
-  if (items <= 1024) return run_rows<T, 4, false>(a, 256, items, s);
-  if (items <= 2048) return run_rows<T, 4, false>(a, 512, items, s);
-  if (items <= 4096) return run_rows<T, 4, false>(a, 1024, items, s);
-  if (items <= 8192) return run_rows<T, 8, false>(a, 1024, items, s);
-  if (items <= 16384) return run_rows<T, 16, false>(a, 1024, items, s);
+  // vectors of a lane, threads, and workgroups that a compute unit holds at once
+  if (items <= 64) return run_rows<T, 1, 64>(a, items, 8, s);
+  if (items <= 128) return run_rows<T, 2, 64>(a, items, 8, s);
+  if (items <= 256) return run_rows<T, 4, 64>(a, items, 6, s);
+  if (items <= 1024) return run_rows<T, 4, 256>(a, items, 6, s);
+  if (items <= 2048) return run_rows<T, 8, 256>(a, items, 4, s);
+  if (items <= 4096) return run_rows<T, 16, 256>(a, items, 4, s);
+  if (items <= 8192) return run_rows<T, 16, 512>(a, items, 2, s);
+  if (items <= 16384) return run_rows<T, 32, 512>(a, items, 1, s);
   const int space = row_space_bytes(a.top, items, a.tail);
   if (space > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(distill_stream<T>),

@@ -458,7 +458,7 @@ void set_slab(NormArgs* a, int groups, int V) {
 }
 
 // Two kernels: as many whole groups as 256 threads have vector columns for (a wider group has 1024), and parts
-// of the pixels for some 1024 workgroups, each of at least 16 rows of threads; the parts of one image stay few enough
+// of the pixels for some 2048 workgroups, each of at least 4 rows of threads; the parts of one image stay few enough
 // for every workgroup of the second kernel to join them (4096 group parts: 64 KB out of the L2).
 void set_parts(NormArgs* a, int x_size) {
   const int V = 16 / x_size;
@@ -466,8 +466,8 @@ void set_parts(NormArgs* a, int x_size) {
   set_slab(a, a->cpg < 256 * V ? 256 * V / a->cpg : 1, V);
   const int rows = a->threads >> a->lanes;
   const int64_t cells = (int64_t)a->N * a->slabs;
-  int64_t parts = (1024 + cells - 1) / cells;
-  const int64_t most = a->P / (16 * rows) > 1 ? a->P / (16 * rows) : 1;
+  int64_t parts = (2048 + cells - 1) / cells;
+  const int64_t most = a->P / (4 * rows) > 1 ? a->P / (4 * rows) : 1;
   parts = parts < most ? parts : most;
   const int64_t joined = 4096 / a->slab > 1 ? 4096 / a->slab : 1;
   parts = parts < joined ? parts : joined;

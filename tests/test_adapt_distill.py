@@ -180,6 +180,29 @@ def test_infinities_and_nan(classes, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("classes", [13, 1001, 9003])
+def test_the_largest_logit_is_found_everywhere(classes, dtype):
+    """One logit so far above the rest, at every place in turn, that any other maximum overflows the exponentials;
+    and rows of negative logits alone."""
+    from paper_2407_02913_amd import adapt
+
+    places = list(range(13)) + [classes - k for k in range(1, 10)] + [classes // 2 + k for k in range(9)]
+    places = sorted({p for p in places if 0 <= p < classes})
+    logits = torch.randn(len(places), classes, generator=torch.Generator().manual_seed(1)).to(dtype)
+    for r, p in enumerate(places):
+        logits[r, p] = 300.0
+    logits[1::3] -= 500.0
+    logits = logits.cuda()
+    index = torch.tensor([[p, (p + 1) % classes, (p + 5) % classes] for p in places], device="cuda")
+    values = torch.tensor([[2.0, 1.0, 0.0]], device="cuda").expand(len(places), 3).contiguous()
+    ones = torch.ones(len(places), device="cuda")
+    got = adapt.distill_loss_and_grad(logits, values, index, temperature=1.0)
+    want = definition(logits, values, index, 1.0, False)
+    check((got[0], got[1]), want, dtype, ones, 1.0)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("classes", [600, 20000])
 def test_the_rest_of_a_certain_student(classes):
     """A student who has all but 1e-9 of its mass on the top: the rest is summed as such, not as a difference."""
