@@ -45,8 +45,30 @@ __device__ __forceinline__ v4f mma(const raw4& a, const raw4& b, v4f acc) {
   }
 }
 
-// Floats of a token's row in the workspace.
-__host__ __device__ inline int row_of(int rank) { return (rank + 7) / 8 * 8; }
+// Floats of a token's row in the workspace, zeros behind the rank: what every form of the second product reads
+// (run_expand: steps of 4 V ranks, a power of two of them, at most 32, 64 or 128 ranks).
+__host__ __device__ inline int row_of(int rank) { return rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+
+// A lane's 16 bytes from the lane that loaded them to the one whose operand they are, and back.  Four neighbouring lanes
+// load (store) 64 contiguous bytes of a row -- lane l piece l % 4 of row l / 4 -- where the matrix instructions have row
+// l % 16 and piece l / 16: as those lie, every lane's 16 bytes would be an access of their own to the cache.
+__device__ __forceinline__ unsigned to_operand(unsigned v) {
+  const int lane = threadIdx.x & 63;
+  return (unsigned)__builtin_amdgcn_ds_bpermute(((lane & 15) * 4 + (lane >> 4)) * 4, (int)v);
+}
+__device__ __forceinline__ float from_operand(float v) {
+  const int lane = threadIdx.x & 63;
+  return __uint_as_float((unsigned)__builtin_amdgcn_ds_bpermute(((lane & 3) * 16 + (lane >> 2)) * 4, (int)__float_as_uint(v)));
+}
+__device__ __forceinline__ raw4 to_operand(const raw4& v) {
+  raw4 r;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const unsigned w = v[d];
+    r[d] = to_operand(w);
+  }
+  return r;
+}
 
 // ---- few tokens ----
 
@@ -107,32 +129,36 @@ __global__ __launch_bounds__(256) void expand_few(const float* h, const int32_t*
 struct Shrink {
   const void* x;
   const void* bank;  // [adapters][rank][inputs]
-  float* h;          // [tokens][row_of(rank)]
+  float* h;          // [tokens][row_of(rank)]: scaled sums, or null
+  bf16* split;       // [tokens][2][row_of(rank)]: the same as the sum of two bfloat16 numbers, or null
   int64_t stride;
   int inputs;
 };
 
-constexpr int kTokens = 32;  // of a shrink's tile
-
-// h of 32 tokens: waves share the inputs in turns of 128 bytes a row, and add up in LDS.  RT: sixteens of the rank.
-template <typename T, int RT, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, const int32_t* ids, int2* range,
-                                                          int tokens, int rank, int adapters) {
-  constexpr int V = kVec<T>, STEP = 4 * V, CHUNK = 2 * STEP;
-  __shared__ v4f sums[WAVES][RT][2][64];
+// h of 16 TT tokens: waves share the inputs in turns of 128 bytes a row, and add up in LDS.  RT: sixteens of the rank.
+// Tiles begin at different inputs: rows are a power of two apart more often than not, and tiles that read the same
+// columns at the same time would keep to a part of the memory's channels.
+template <typename T, int RT, int TT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, const int32_t* ids, const float* scale,
+                                                          int2* range, int tokens, int rank, int adapters) {
+  constexpr int V = kVec<T>, STEP = 4 * V, CHUNK = 2 * STEP, TOKENS = 16 * TT;
+  constexpr uint64_t ALL = (1ull << TOKENS) - 1;
+  __shared__ v4f sums[WAVES][RT][TT][64];
   const Shrink p = blockIdx.y ? p1 : p0;
-  const int t0 = blockIdx.x * kTokens, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = lane & 15, group = lane >> 4;
+  const int t0 = blockIdx.x * TOKENS, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int row = lane >> 2, group = lane & 3;  // as loaded (to_operand)
   const T* x = static_cast<const T*>(p.x);
   const int64_t end_x = (tokens - 1) * p.stride + p.inputs, end_w = (int64_t)adapters * rank * p.inputs;
-  int64_t at_x[2];
+  int64_t at_x[TT];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) at_x[i] = min(t0 + 16 * i + row, tokens - 1) * p.stride + group * V;
-  const int mine = t0 + (lane & 31) < tokens ? ids[t0 + (lane & 31)] : -1;
-  uint64_t left = __ballot(lane < kTokens && mine >= 0 && mine < adapters);
+  for (int i = 0; i < TT; ++i) at_x[i] = min(t0 + 16 * i + row, tokens - 1) * p.stride + group * V;
+  const int mine = t0 + (lane & (TOKENS - 1)) < tokens ? ids[t0 + (lane & (TOKENS - 1))] : -1;
+  uint64_t left = __ballot(mine >= 0 && mine < adapters) & ALL;
+  const int chunks = p.inputs / CHUNK, turn = (int)(blockIdx.x * WAVES % (unsigned)max(chunks, 1));
   while (left) {  // (the same in every wave of the workgroup)
     const int l = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-    const uint64_t sel = __ballot(lane < kTokens && mine == l);
+    const uint64_t sel = __ballot(mine == l) & ALL;
     left &= ~sel;
     if (range && blockIdx.y == 0 && threadIdx.x == 0) {
       atomicMin(&range[l].x, t0 + (int)__builtin_ctzll(sel));
@@ -142,96 +168,119 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, 
     int64_t at_w[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) at_w[r] = ((int64_t)l * rank + min(16 * r + row, rank - 1)) * p.inputs + group * V;
-    v4f acc[RT][2];
+    v4f acc[RT][TT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) acc[r][0] = acc[r][1] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    const int whole = p.inputs / CHUNK * CHUNK;
-    for (int k = wave * CHUNK; k < whole; k += WAVES * CHUNK) {
-      raw4 a[2][2], b[2][RT];
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < TT; ++i) acc[r][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = wave; c < chunks; c += WAVES) {
+      const int from = c + turn, k = (from < chunks ? from : from - chunks) * CHUNK;
+      raw4 a[2][TT], b[2][RT];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) a[u][i] = load16(x + at_x[i] + k + u * STEP);
+        for (int i = 0; i < TT; ++i) a[u][i] = load16(x + at_x[i] + k + u * STEP);
 #pragma unroll
         for (int r = 0; r < RT; ++r) b[u][r] = load16(w + at_w[r] + k + u * STEP);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int i = 0; i < TT; ++i) a[u][i] = to_operand(a[u][i]);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[r][i] = mma<T>(b[u][r], a[u][i], acc[r][i]);
+        for (int r = 0; r < RT; ++r) {
+          b[u][r] = to_operand(b[u][r]);
+#pragma unroll
+          for (int i = 0; i < TT; ++i) acc[r][i] = mma<T>(b[u][r], a[u][i], acc[r][i]);
+        }
+      }
     }
-    if (wave == (whole / CHUNK) % WAVES) {  // what is left of the inputs, cut on both sides
-      for (int k = whole; k < p.inputs; k += STEP) {
+    if (wave == chunks % WAVES) {  // what is left of the inputs, cut on both sides
+      for (int k = chunks * CHUNK; k < p.inputs; k += STEP) {
         const int valid = p.inputs - k - group * V;
-        raw4 a[2], b[RT];
+        raw4 a[TT], b[RT];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < TT; ++i)
           a[i] = valid > 0 ? load_cut(x + at_x[i] + k, valid, end_x - at_x[i] - k) : raw4{0u, 0u, 0u, 0u};
 #pragma unroll
         for (int r = 0; r < RT; ++r)
           b[r] = valid > 0 ? load_cut(w + at_w[r] + k, valid, end_w - at_w[r] - k) : raw4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+        for (int i = 0; i < TT; ++i) a[i] = to_operand(a[i]);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) acc[r][i] = mma<T>(b[r], a[i], acc[r][i]);
+        for (int r = 0; r < RT; ++r) {
+          b[r] = to_operand(b[r]);
+#pragma unroll
+          for (int i = 0; i < TT; ++i) acc[r][i] = mma<T>(b[r], a[i], acc[r][i]);
+        }
       }
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sums[wave][r][i][lane] = acc[r][i];
+      for (int i = 0; i < TT; ++i) sums[wave][r][i][lane] = acc[r][i];
     __syncthreads();
-    for (int s = threadIdx.x; s < RT * 2 * 64; s += WAVES * 64) {
-      const int r = s >> 7, i = s >> 6 & 1, ln = s & 63, t = 16 * i + (ln & 15), first = 16 * r + 4 * (ln >> 4);
-      v4f v = sums[0][r][i][ln];
+    const float f = scale ? scale[l] : 1.0f;
+    const int quads = row_of(rank) / 4;
+    for (int s = threadIdx.x; s < quads * TOKENS; s += WAVES * 64) {
+      const int t = s / quads, first = (s - t * quads) * 4, r = first >> 4, ln = (first >> 2 & 3) * 16 + (t & 15);
+      if (!(sel >> t & 1)) continue;
+      v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (r < RT) {
 #pragma unroll
-      for (int q = 1; q < WAVES; ++q) v += sums[q][r][i][ln];
-      if ((sel >> t & 1) && first < rank)
-        *reinterpret_cast<v4f*>(p.h + (int64_t)(t0 + t) * row_of(rank) + first) = v;
+        for (int q = 0; q < WAVES; ++q) v += sums[q][r][t >> 4][ln];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = first + e < rank ? v[e] * f : 0.0f;
+      if (p.h) *reinterpret_cast<v4f*>(p.h + (int64_t)(t0 + t) * row_of(rank) + first) = v;
+      if (p.split) {
+        typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          hi[e] = (bf16)v[e];
+          const float rest = v[e] - (float)hi[e];
+          lo[e] = (bf16)(rest == rest ? rest : 0.0f);  // (an infinity leaves no rest)
+        }
+        bf16* to = p.split + (int64_t)(t0 + t) * 2 * row_of(rank) + first;
+        *reinterpret_cast<bf16x4*>(to) = hi;
+        *reinterpret_cast<bf16x4*>(to + row_of(rank)) = lo;
+      }
     }
     __syncthreads();
   }
 }
 
-// Ranks [r0, r0 + V) of a token's h, zeros past the rank.
-template <int V>
-__device__ __forceinline__ void load_h(const float* h, int r0, int rank, bool live, float (&v)[V]) {
-#pragma unroll
-  for (int j = 0; j < V; j += 4) {
-    const bool there = live && r0 + j < rank;
-    const v4f q = there ? *reinterpret_cast<const v4f*>(h + r0 + j) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[j + e] = r0 + j + e < rank ? q[e] : 0.0f;
-  }
-}
-
-// acc += a h of one step: a is a vector of the bank's row, h its floats.  bfloat16: h as the sum of two numbers, which
-// keeps 16 of its 24 bits at two instructions; float16: in float32, since h may leave its range.
+// A step's part of a token's h as the second product takes it: bfloat16 as the sum of two numbers, which keeps 16 of its
+// 24 bits at two instructions; else in float32, whose range float16 would leave.
 template <typename T>
-__device__ __forceinline__ v4f mma_h(const raw4& a, const float (&h)[kVec<T>], v4f acc) {
-  if constexpr (__is_same(T, bf16)) {
-    bf16x8 hi, lo;
+struct HPart {
+  v4f v[kVec<T> / 4];
+  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at, bool live) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi[j] = (bf16)h[j];
-      const float rest = h[j] - (float)hi[j];
-      lo[j] = (bf16)(rest == rest ? rest : 0.0f);  // (an infinity leaves no rest)
-    }
-    const bf16x8 w = __builtin_bit_cast(bf16x8, a);
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, lo, acc, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, hi, acc, 0, 0, 0);
-  } else {
+    for (int j = 0; j < kVec<T> / 4; ++j)
+      v[j] = live ? *reinterpret_cast<const v4f*>(h + t * row + at + 4 * j) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  __device__ __forceinline__ v4f times(const raw4& w, v4f acc) const {
 #pragma unroll
     for (int j = 0; j < kVec<T>; ++j)
-      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T>(a, j), h[j], acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(element<T>(w, j), v[j / 4][j % 4], acc, 0, 0, 0);
     return acc;
   }
-}
+};
+template <>
+struct HPart<bf16> {
+  raw4 hi, lo;
+  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at, bool live) {
+    const bf16* from = reinterpret_cast<const bf16*>(h) + t * 2 * row + at;
+    hi = lo = raw4{0u, 0u, 0u, 0u};
+    if (live) hi = load16(from), lo = load16(from + row);
+  }
+  __device__ __forceinline__ v4f times(const raw4& w, v4f acc) const { return mma<bf16>(w, hi, mma<bf16>(w, lo, acc)); }
+};
 
 struct Expand {
-  const float* h;
+  const float* h;    // Shrink::h, bfloat16 Shrink::split
   const void* bank;  // [adapters][outputs][rank]
   const void* base;
   void* y;
@@ -239,47 +288,63 @@ struct Expand {
   int outputs;
 };
 
-// y of 64 outputs a wave over a run of tokens, sixteen at a time; the bank's rows stay in registers while the adapter
-// stays.  STEPS: of 4 V ranks.
+// y of 64 outputs a wave over a run of tokens, sixteen at a time, the next sixteen's values on their way; the bank's rows
+// stay in registers while the adapter stays.  STEPS: of 4 V ranks.  Neighbouring workgroups take neighbouring outputs of
+// the same tokens.
 template <typename T, int STEPS>
-__global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids, const float* scale, int tokens, int rank,
-                                                   int adapters, int run) {
+__global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids, int tokens, int rank, int adapters, int run,
+                                                   int across) {
   constexpr int V = kVec<T>, PARTS = 16 / V;  // 16-byte pieces of a lane's outputs
   const int lane = threadIdx.x & 63, row = lane & 15, group = lane >> 4;
-  const int m0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 64;
+  const int nth = blockIdx.x / across;
+  const int m0 = ((blockIdx.x - nth * across) * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * 64;
   if (m0 >= p.outputs) return;
   const T* bank = static_cast<const T*>(p.bank);
   const T* base = static_cast<const T*>(p.base);
   T* y = static_cast<T*>(p.y);
   const int64_t end_w = (int64_t)adapters * p.outputs * rank;
   const int64_t end_base = (tokens - 1) * p.base_stride + p.outputs;
+  const int h_row = row_of(rank);
   // Tile a's row i is output m0 + place(a, i): a lane's four results of tiles that belong together are then
   // neighbours, V of them a piece, and four lane groups' pieces 64 bytes of a token's row.
   auto place = [](int a, int i) { return (a * 4 / V) * 4 * V + (i >> 2) * V + (a * 4) % V + (i & 3); };
-  raw4 w[4][STEPS];
-  int loaded = -1;
-  const int first = blockIdx.x * run, last = min(tokens, first + run);
-  for (int t0 = first; t0 < last; t0 += 16) {
-    const int t = t0 + row;
-    const bool live = t < last;
-    const int mine = live ? ids[t] : -1;
+  struct Values {
+    int id;
     raw4 old[PARTS];
+    HPart<T> h[STEPS];
+  };
+  const int first = nth * run, last = min(tokens, first + run);
+  // (base and y: piece lane % 4 of token lane / 4; the rest: token lane % 16)
+  const int own = lane >> 2, m_own = m0 + (lane & 3) * V;
+  auto fetch = [&](int t0) {
+    Values v;
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const int m = m0 + q * 4 * V + group * V;
-      old[q] = raw4{0u, 0u, 0u, 0u};
-      if (base && live && m < p.outputs) {
-        const int64_t at = t * p.base_stride + m;
-        old[q] = load_cut(base + at, p.outputs - m, end_base - at);
+      const int m = m_own + q * 4 * V;
+      v.old[q] = raw4{0u, 0u, 0u, 0u};
+      if (base && t0 + own < last && m < p.outputs) {
+        const int64_t at = (t0 + own) * p.base_stride + m;
+        v.old[q] = load_cut(base + at, p.outputs - m, end_base - at);
       }
     }
+    v.id = t0 + row < last ? ids[t0 + row] : -1;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) v.h[s].load(p.h, t0 + row, h_row, (s * 4 + group) * V, t0 + row < last);
+    return v;
+  };
+  raw4 w[4][STEPS];
+  int loaded = -1;
+  Values next = fetch(first);
+  for (int t0 = first; t0 < last; t0 += 16) {
+    const Values now = next;
+    next = fetch(t0 + 16);
     v4f acc[4];
 #pragma unroll
     for (int a = 0; a < 4; ++a) acc[a] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    uint64_t left = __ballot(lane < 16 && mine >= 0 && mine < adapters);
+    uint64_t left = __ballot(now.id >= 0 && now.id < adapters) & 0xffffu;
     while (left) {
-      const int l = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
-      left &= ~__ballot(lane < 16 && mine == l);
+      const int l = __builtin_amdgcn_readlane(now.id, __builtin_ctzll(left));
+      left &= ~__ballot(now.id == l);
       if (l != loaded) {
         loaded = l;
 #pragma unroll
@@ -291,32 +356,27 @@ __global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids,
             w[a][s] = m < p.outputs && r < rank ? load_cut(bank + at, rank - r, end_w - at) : raw4{0u, 0u, 0u, 0u};
           }
       }
-      v4f own[4];
+      v4f own_acc[4];
 #pragma unroll
-      for (int a = 0; a < 4; ++a) own[a] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int a = 0; a < 4; ++a) {
+        own_acc[a] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        float h[V];
-        load_h<V>(p.h + (int64_t)t * row_of(rank), (s * 4 + group) * V, rank, mine == l, h);
-#pragma unroll
-        for (int a = 0; a < 4; ++a) own[a] = mma_h<T>(w[a][s], h, own[a]);
+        for (int s = 0; s < STEPS; ++s) own_acc[a] = now.h[s].times(w[a][s], own_acc[a]);
       }
-      // (chosen, not multiplied by zero: an adapter that holds infinities is no matter of the other tokens)
-      if (mine == l) {
+      // A token is a column of its own.  (Chosen, not multiplied by zero: an adapter that holds infinities is no matter of
+      // the other tokens, nor is what the workspace holds for a token without one.)
+      if (now.id == l) {
 #pragma unroll
-        for (int a = 0; a < 4; ++a) acc[a] = own[a];
+        for (int a = 0; a < 4; ++a) acc[a] = own_acc[a];
       }
     }
-    const float f = mine < 0 || mine >= adapters ? 0.0f : scale ? scale[mine] : 1.0f;
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const int m = m0 + q * 4 * V + group * V;
-      if (live && m < p.outputs) {
-        float v[V];
+      const int m = m_own + q * 4 * V;
+      float v[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = fmaf(f, acc[q * V / 4 + j / 4][j % 4], element<T>(old[q], j));
-        store_vec<T, V>(y + t * p.y_stride + m, v, p.outputs - m);
-      }
+      for (int j = 0; j < V; ++j) v[j] = from_operand(acc[q * V / 4 + j / 4][j % 4]) + element<T>(now.old[q], j);
+      if (t0 + own < last && m < p.outputs) store_vec<T, V>(y + (t0 + own) * p.y_stride + m, v, p.outputs - m);
     }
   }
 }
@@ -445,41 +505,52 @@ __global__ __launch_bounds__(256) void outer_tile(Outer p0, Outer p1, const int3
   }
 }
 
-// Adds the splits, scales, rounds: d down as it lies, d up transposed.
+// Adds the splits, rounds: d down as it lies, d up transposed.
 template <typename T>
-__global__ __launch_bounds__(256) void outer_finish(const float* part_down, const float* part_up, const float* scale, T* d_down,
-                                                    T* d_up, int rank, int inputs, int outputs, int adapters, int splits,
+__global__ __launch_bounds__(256) void outer_finish(const float* part_down, const float* part_up, T* d_down, T* d_up,
+                                                    int rank, int inputs, int outputs, int adapters, int splits,
                                                     int blocks_down, int blocks_up) {
   const bool second = (int)blockIdx.x >= blocks_down * adapters;
   const int id = second ? blockIdx.x - blocks_down * adapters : blockIdx.x;
   const int blocks = second ? blocks_up : blocks_down, cols = second ? outputs : inputs;
   const int l = id / blocks, c = (id - l * blocks) * 256 + threadIdx.x;
   if (c >= cols) return;
-  const float f = scale ? scale[l] : 1.0f;
   const int64_t split = (int64_t)adapters * rank * cols;
   const float* from = (second ? part_up : part_down) + (int64_t)l * rank * cols + c;
   for (int r = blockIdx.y; r < rank; r += gridDim.y) {
     float v = 0.0f;
+#pragma unroll 8
     for (int s = 0; s < splits; ++s) v += from[s * split + (int64_t)r * cols];
-    if (second) d_up[((int64_t)l * outputs + c) * rank + r] = (T)(v * f);
-    else d_down[((int64_t)l * rank + r) * inputs + c] = (T)(v * f);
+    if (second) d_up[((int64_t)l * outputs + c) * rank + r] = (T)v;
+    else d_down[((int64_t)l * rank + r) * inputs + c] = (T)v;
   }
 }
 
 size_t up64(size_t v) { return (v + 63) / 64 * 64; }
 
-template <typename T, int RT, int WAVES>
+template <typename T, int RT, int TT, int WAVES>
 void run_shrink_as(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
-  const dim3 grid((unsigned)((a.tokens + kTokens - 1) / kTokens), (unsigned)products);
-  shrink_tile<T, RT, WAVES><<<grid, WAVES * 64, 0, s>>>(p0, p1, a.ids, range, a.tokens, a.rank, a.adapters);
+  const dim3 grid((unsigned)((a.tokens + 16 * TT - 1) / (16 * TT)), (unsigned)products);
+  shrink_tile<T, RT, TT, WAVES><<<grid, WAVES * 64, 0, s>>>(p0, p1, a.ids, a.scale, range, a.tokens, a.rank, a.adapters);
 }
 
 template <typename T>
 hipError_t run_shrink(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
-  if (a.rank <= 16) run_shrink_as<T, 1, 8>(p0, p1, products, a, range, s);
-  else if (a.rank <= 32) run_shrink_as<T, 2, 8>(p0, p1, products, a, range, s);
-  else if (a.rank <= 64) run_shrink_as<T, 4, 4>(p0, p1, products, a, range, s);
-  else run_shrink_as<T, 8, 4>(p0, p1, products, a, range, s);
+  // (tiles of 16 tokens where 32 would leave compute units without a workgroup)
+  const bool small = (int64_t)products * a.tokens < 32 * 512;
+  if (a.rank <= 16) {
+    if (small) run_shrink_as<T, 1, 1, 8>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 1, 2, 8>(p0, p1, products, a, range, s);
+  } else if (a.rank <= 32) {
+    if (small) run_shrink_as<T, 2, 1, 8>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 2, 2, 8>(p0, p1, products, a, range, s);
+  } else if (a.rank <= 64) {
+    if (small) run_shrink_as<T, 4, 1, 8>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 4, 2, 4>(p0, p1, products, a, range, s);
+  } else {
+    if (small) run_shrink_as<T, 8, 1, 4>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 8, 2, 4>(p0, p1, products, a, range, s);
+  }
   return hipGetLastError();
 }
 
@@ -489,14 +560,21 @@ hipError_t run_expand(const Expand& p, const LowrankArgs& a, hipStream_t s) {
   const int across = (p.outputs + 255) / 256;
   int run = (int)(((int64_t)a.tokens * across + 2047) / 2048);
   run = (run + 15) / 16 * 16;
-  const dim3 grid((unsigned)((a.tokens + run - 1) / run), (unsigned)across);
+  const dim3 grid((unsigned)((a.tokens + run - 1) / run * across));
   const int steps = (a.rank + 4 * kVec<T> - 1) / (4 * kVec<T>);
-  if (steps <= 1) expand_tile<T, 1><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
-  else if (steps <= 2) expand_tile<T, 2><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
-  else if (steps <= 4) expand_tile<T, 4><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+  if (steps <= 1) expand_tile<T, 1><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
+  else if (steps <= 2) expand_tile<T, 2><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
+  else if (steps <= 4) expand_tile<T, 4><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
   else if constexpr (sizeof(T) == 4)
-    expand_tile<T, 8><<<grid, 256, 0, s>>>(p, a.ids, a.scale, a.tokens, a.rank, a.adapters, run);
+    expand_tile<T, 8><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
   return hipGetLastError();
+}
+
+// A shrink whose result an expand takes.
+template <typename T>
+Shrink shrink_of(const void* x, const void* bank, void* h, int64_t stride, int inputs) {
+  if constexpr (__is_same(T, bf16)) return Shrink{x, bank, nullptr, static_cast<bf16*>(h), stride, inputs};
+  return Shrink{x, bank, static_cast<float*>(h), nullptr, stride, inputs};
 }
 
 template <typename T>
@@ -511,7 +589,7 @@ hipError_t run_lowrank(const LowrankArgs& a, hipStream_t s) {
         static_cast<T*>(a.y), a.y_stride, a.outputs, a.rank, a.adapters);
     return hipGetLastError();
   }
-  const Shrink p{a.x, a.down, h, a.x_stride, a.inputs};
+  const Shrink p = shrink_of<T>(a.x, a.down, a.space, a.x_stride, a.inputs);
   const hipError_t e = run_shrink<T>(p, p, 1, a, nullptr, s);
   if (e != hipSuccess) return e;
   return run_expand<T>(Expand{h, a.up, a.base, a.y, a.base_stride, a.y_stride, a.outputs}, a, s);
@@ -520,7 +598,7 @@ hipError_t run_lowrank(const LowrankArgs& a, hipStream_t s) {
 // The backward call's workspace.
 struct BackwardPlan {
   int splits, blocks_down, blocks_up;
-  size_t h, g, down_t, up_t, range, part_down, part_up, bytes;
+  size_t h, g, split, down_t, up_t, range, part_down, part_up, bytes;
 };
 
 BackwardPlan plan_backward(const LowrankArgs& a, int size) {
@@ -543,6 +621,7 @@ BackwardPlan plan_backward(const LowrankArgs& a, int size) {
   };
   b.h = take(rows);
   b.g = take(rows);
+  b.split = take(size == 2 ? rows : 0);
   b.down_t = take(down * size);
   b.up_t = take(up * size);
   b.range = take((size_t)a.adapters * 8);
@@ -561,8 +640,8 @@ void run_outer(const Outer& p0, const Outer& p1, const LowrankArgs& a, const int
 template <typename T>
 hipError_t run_finish(const LowrankArgs& a, const float* part_down, const float* part_up, int splits, hipStream_t s) {
   const int down = (a.inputs + 255) / 256, up = (a.outputs + 255) / 256;
-  const dim3 grid((unsigned)((down + up) * a.adapters), (unsigned)((a.rank + 3) / 4));
-  outer_finish<T><<<grid, 256, 0, s>>>(part_down, part_up, a.scale, static_cast<T*>(a.d_down), static_cast<T*>(a.d_up), a.rank,
+  const dim3 grid((unsigned)((down + up) * a.adapters), (unsigned)a.rank);
+  outer_finish<T><<<grid, 256, 0, s>>>(part_down, part_up, static_cast<T*>(a.d_down), static_cast<T*>(a.d_up), a.rank,
                                        a.inputs, a.outputs, a.adapters, splits, down, up);
   return hipGetLastError();
 }
@@ -582,10 +661,12 @@ hipError_t run_lowrank_backward(const LowrankArgs& a, hipStream_t s) {
       static_cast<const T*>(a.down), down_t, static_cast<const T*>(a.up), up_t, range, a.adapters, a.rank, a.inputs, a.outputs,
       tiles_down, tiles_up);
   // h = x down^T and g = dy up
-  hipError_t e = run_shrink<T>(Shrink{a.x, a.down, h, a.x_stride, a.inputs}, Shrink{a.dy, up_t, g, a.dy_stride, a.outputs}, 2,
-                               a, range, s);
+  const bool split = __is_same(T, bf16);
+  bf16* both = split ? reinterpret_cast<bf16*>(a.space + b.split) : nullptr;
+  hipError_t e = run_shrink<T>(Shrink{a.x, a.down, h, nullptr, a.x_stride, a.inputs},
+                               Shrink{a.dy, up_t, g, both, a.dy_stride, a.outputs}, 2, a, range, s);
   if (e != hipSuccess) return e;
-  e = run_expand<T>(Expand{g, down_t, a.base, a.y, a.base_stride, a.y_stride, a.inputs}, a, s);
+  e = run_expand<T>(Expand{split ? reinterpret_cast<float*>(both) : g, down_t, a.base, a.y, a.base_stride, a.y_stride, a.inputs}, a, s);
   if (e != hipSuccess) return e;
   const Outer p0{g, a.x, part_down, a.x_stride, a.inputs, b.blocks_down};
   const Outer p1{h, a.dy, part_up, a.dy_stride, a.outputs, b.blocks_up};
