@@ -439,7 +439,11 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? 4 : NV == 8 ?
       for (int u = 0; u < NV; ++u) {
         if (u <= full) {
           gradient<T>(a, r, unit, raw[u], v);
-          if (u < full || lane < ragged) store_vec<T, V>(grad + u * LANES * V + offset, v, V);
+          if (u < full || lane < ragged) {
+            T* to = grad + u * LANES * V + offset;
+            if (a.stream) store_vec<T, V, true>(to, v, V);
+            else store_vec<T, V>(to, v, V);
+          }
           raw[u] = load(next_at, u);
         }
       }

@@ -17,6 +17,7 @@ struct DistillArgs {
   int64_t logits_stride, grad_stride, values_stride, index_stride;
   bool wide, tail;         // int64 places; the rest of the mass as one more outcome
   float temperature;
+  bool stream;             // the gradient is stored past the caches
 };
 
 // loss: from the logits (with stats if given); grad alone: from stats.  type: sfc_type.

@@ -40,6 +40,7 @@ sfc_status run(const sfc_distill_desc* d, const void* logits, const float* value
   a.wide = d->index_wide != 0;
   a.tail = d->tail != 0;
   a.temperature = d->temperature;
+  a.stream = d->rows * d->classes * size >= sfc::kStreamBytes;
   return sfc::launch_distill(a, d->type, static_cast<hipStream_t>(stream)) == hipSuccess ? SFC_OK : SFC_EHIP;
 }
 

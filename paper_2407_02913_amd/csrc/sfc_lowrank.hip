@@ -45,20 +45,23 @@ __device__ __forceinline__ v4f mma(const raw4& a, const raw4& b, v4f acc) {
   }
 }
 
+// LDS accesses of a wave's lanes on either side stay in their order.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Floats of a token's row in the workspace, zeros behind the rank: what every form of the second product reads
 // (run_expand: steps of 4 V ranks, a power of two of them, at most 32, 64 or 128 ranks).
 __host__ __device__ inline int row_of(int rank) { return rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 
-// A lane's 16 bytes from the lane that loaded them to the one whose operand they are, and back.  Four neighbouring lanes
-// load (store) 64 contiguous bytes of a row -- lane l piece l % 4 of row l / 4 -- where the matrix instructions have row
-// l % 16 and piece l / 16: as those lie, every lane's 16 bytes would be an access of their own to the cache.
+// A lane's 16 bytes from the lane that loaded them to the one whose operand they are.  Four neighbouring lanes load 64
+// contiguous bytes of a row -- lane l piece l % 4 of row l / 4 -- where the matrix instructions have row l % 16 and piece
+// l / 16: as those lie, every lane's 16 bytes would be an access of their own to the cache.
 __device__ __forceinline__ unsigned to_operand(unsigned v) {
   const int lane = threadIdx.x & 63;
   return (unsigned)__builtin_amdgcn_ds_bpermute(((lane & 15) * 4 + (lane >> 4)) * 4, (int)v);
-}
-__device__ __forceinline__ float from_operand(float v) {
-  const int lane = threadIdx.x & 63;
-  return __uint_as_float((unsigned)__builtin_amdgcn_ds_bpermute(((lane & 3) * 16 + (lane >> 2)) * 4, (int)__float_as_uint(v)));
 }
 __device__ __forceinline__ raw4 to_operand(const raw4& v) {
   raw4 r;
@@ -256,10 +259,9 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, 
 template <typename T>
 struct HPart {
   v4f v[kVec<T> / 4];
-  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at, bool live) {
+  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at) {
 #pragma unroll
-    for (int j = 0; j < kVec<T> / 4; ++j)
-      v[j] = live ? *reinterpret_cast<const v4f*>(h + t * row + at + 4 * j) : v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < kVec<T> / 4; ++j) v[j] = *reinterpret_cast<const v4f*>(h + t * row + at + 4 * j);
   }
   __device__ __forceinline__ v4f times(const raw4& w, v4f acc) const {
 #pragma unroll
@@ -271,10 +273,9 @@ struct HPart {
 template <>
 struct HPart<bf16> {
   raw4 hi, lo;
-  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at, bool live) {
+  __device__ __forceinline__ void load(const float* h, int64_t t, int row, int at) {
     const bf16* from = reinterpret_cast<const bf16*>(h) + t * 2 * row + at;
-    hi = lo = raw4{0u, 0u, 0u, 0u};
-    if (live) hi = load16(from), lo = load16(from + row);
+    hi = load16(from), lo = load16(from + row);
   }
   __device__ __forceinline__ v4f times(const raw4& w, v4f acc) const { return mma<bf16>(w, hi, mma<bf16>(w, lo, acc)); }
 };
@@ -289,47 +290,50 @@ struct Expand {
 };
 
 // y of 64 outputs a wave over a run of tokens, sixteen at a time, the next sixteen's values on their way; the bank's rows
-// stay in registers while the adapter stays.  STEPS: of 4 V ranks.  Neighbouring workgroups take neighbouring outputs of
-// the same tokens.
-template <typename T, int STEPS>
+// stay in registers while the adapter stays.  STEPS: of 4 V ranks.  Results pass through LDS, so that a wave loads and
+// stores whole 128 (float32: 256) bytes of a token's row.  Neighbouring workgroups take neighbouring outputs of the same
+// tokens.
+template <typename T, int STEPS, bool STREAM>
 __global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids, int tokens, int rank, int adapters, int run,
                                                    int across) {
-  constexpr int V = kVec<T>, PARTS = 16 / V;  // 16-byte pieces of a lane's outputs
+  constexpr int V = kVec<T>, PARTS = 16 / V, PER = 64 / V, PITCH = 68;  // PER: lanes for a token's 64 outputs
+  __shared__ float tiles[4][16 * PITCH];
   const int lane = threadIdx.x & 63, row = lane & 15, group = lane >> 4;
-  const int nth = blockIdx.x / across;
-  const int m0 = ((blockIdx.x - nth * across) * 4 + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) * 64;
-  if (m0 >= p.outputs) return;
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int nth = blockIdx.x / across, m0 = ((blockIdx.x - nth * across) * 4 + wave) * 64;
+  if (m0 >= p.outputs) return;  // (waves share nothing)
+  float* tile = tiles[wave];
   const T* bank = static_cast<const T*>(p.bank);
   const T* base = static_cast<const T*>(p.base);
   T* y = static_cast<T*>(p.y);
   const int64_t end_w = (int64_t)adapters * p.outputs * rank;
   const int64_t end_base = (tokens - 1) * p.base_stride + p.outputs;
   const int h_row = row_of(rank);
-  // Tile a's row i is output m0 + place(a, i): a lane's four results of tiles that belong together are then
-  // neighbours, V of them a piece, and four lane groups' pieces 64 bytes of a token's row.
-  auto place = [](int a, int i) { return (a * 4 / V) * 4 * V + (i >> 2) * V + (a * 4) % V + (i & 3); };
   struct Values {
     int id;
     raw4 old[PARTS];
     HPart<T> h[STEPS];
   };
   const int first = nth * run, last = min(tokens, first + run);
-  // (base and y: piece lane % 4 of token lane / 4; the rest: token lane % 16)
-  const int own = lane >> 2, m_own = m0 + (lane & 3) * V;
+  const bool whole = m0 + 64 <= p.outputs;
+  // base and y: V outputs from m on of token t0 + own, own + V, ...; ids and h: token t0 + lane % 16.  (Tokens behind the
+  // run read the last one's values, and store nothing.)
+  const int own = lane / PER, m = m0 + lane % PER * V;
   auto fetch = [&](int t0) {
     Values v;
 #pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const int m = m_own + q * 4 * V;
+      const int64_t at = min(t0 + q * V + own, last - 1) * p.base_stride + m;
       v.old[q] = raw4{0u, 0u, 0u, 0u};
-      if (base && t0 + own < last && m < p.outputs) {
-        const int64_t at = (t0 + own) * p.base_stride + m;
-        v.old[q] = load_cut(base + at, p.outputs - m, end_base - at);
+      if (base) {
+        if (whole) v.old[q] = load16(base + at);
+        else if (m < p.outputs) v.old[q] = load_cut(base + at, p.outputs - m, end_base - at);
       }
     }
-    v.id = t0 + row < last ? ids[t0 + row] : -1;
+    const int t = min(t0 + row, last - 1);
+    v.id = t0 + row < last ? ids[t] : -1;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) v.h[s].load(p.h, t0 + row, h_row, (s * 4 + group) * V, t0 + row < last);
+    for (int s = 0; s < STEPS; ++s) v.h[s].load(p.h, t, h_row, (s * 4 + group) * V);
     return v;
   };
   raw4 w[4][STEPS];
@@ -351,9 +355,9 @@ __global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids,
         for (int a = 0; a < 4; ++a)
 #pragma unroll
           for (int s = 0; s < STEPS; ++s) {
-            const int m = m0 + place(a, row), r = (s * 4 + group) * V;
-            const int64_t at = ((int64_t)l * p.outputs + m) * rank + r;
-            w[a][s] = m < p.outputs && r < rank ? load_cut(bank + at, rank - r, end_w - at) : raw4{0u, 0u, 0u, 0u};
+            const int o = m0 + 16 * a + row, r = (s * 4 + group) * V;
+            const int64_t at = ((int64_t)l * p.outputs + o) * rank + r;
+            w[a][s] = o < p.outputs && r < rank ? load_cut(bank + at, rank - r, end_w - at) : raw4{0u, 0u, 0u, 0u};
           }
       }
       v4f own_acc[4];
@@ -371,13 +375,26 @@ __global__ __launch_bounds__(256) void expand_tile(Expand p, const int32_t* ids,
       }
     }
 #pragma unroll
+    for (int a = 0; a < 4; ++a) *reinterpret_cast<v4f*>(tile + row * PITCH + 16 * a + 4 * group) = acc[a];
+    wave_order();
+#pragma unroll
     for (int q = 0; q < PARTS; ++q) {
-      const int m = m_own + q * 4 * V;
+      const int t = t0 + q * V + own;
+      const float* from = tile + (q * V + own) * PITCH + lane % PER * V;
       float v[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = from_operand(acc[q * V / 4 + j / 4][j % 4]) + element<T>(now.old[q], j);
-      if (t0 + own < last && m < p.outputs) store_vec<T, V>(y + (t0 + own) * p.y_stride + m, v, p.outputs - m);
+      for (int j = 0; j < V; j += 4) {
+        const v4f f = *reinterpret_cast<const v4f*>(from + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[j + e] = f[e] + element<T>(now.old[q], j + e);
+      }
+      if (t < last) {
+        T* to = y + t * p.y_stride + m;
+        if (whole) store_vec<T, V, STREAM>(to, v, V);
+        else if (m < p.outputs) store_vec<T, V, STREAM>(to, v, p.outputs - m);
+      }
     }
+    wave_order();
   }
 }
 
@@ -398,11 +415,15 @@ __global__ __launch_bounds__(256) void transpose_banks(const T* down, T* down_t,
   const int r0 = tl / across * 64, c0 = tl % across * 64;
   const T* from = (first ? down : up) + (int64_t)l * rows * cols;
   T* to = (first ? down_t : up_t) + (int64_t)l * rows * cols;
-  const int c = threadIdx.x & 63;
-  for (int r = threadIdx.x >> 6; r < 64; r += 4)
-    if (r0 + r < rows && c0 + c < cols) tile[r][c] = from[(int64_t)(r0 + r) * cols + c0 + c];
+  const int c = threadIdx.x & 63, r4 = threadIdx.x >> 6;
+  T v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i)  // (a place behind the edge reads the last one within)
+    v[i] = from[(int64_t)min(r0 + r4 + 4 * i, rows - 1) * cols + min(c0 + c, cols - 1)];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) tile[r4 + 4 * i][c] = v[i];
   __syncthreads();
-  for (int r = threadIdx.x >> 6; r < 64; r += 4)
+  for (int r = r4; r < 64; r += 4)
     if (c0 + r < cols && r0 + c < rows) to[(int64_t)(c0 + r) * rows + r0 + c] = tile[c][r];
 }
 
@@ -443,17 +464,23 @@ __global__ __launch_bounds__(256) void outer_tile(Outer p0, Outer p1, const int3
     for (int t0 = first + wave * 16; t0 < last; t0 += 64) {
       raw4 xv[4];
       float gv[4][RT];
+      int id[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int t = t0 + u * 4 + group;
-        const bool mine = t < last && ids[t] == l;
-        xv[u] = raw4{0u, 0u, 0u, 0u};
-        if (mine && c < p.cols) xv[u] = load_cut(x + t * p.stride + c, p.cols - c, end_x - t * p.stride - c);
+        // (tokens behind the part's last one, and those of other adapters, are read and dropped)
+        const int t = min(t0 + u * 4 + group, last - 1);
+        id[u] = t0 + u * 4 + group < last ? ids[t] : -1;
+        xv[u] = c < p.cols ? load_cut(x + t * p.stride + c, p.cols - c, end_x - t * p.stride - c) : raw4{0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const int at = r0 + r * 16 + row;
-          gv[u][r] = mine && at < rank ? p.g[(int64_t)t * h_row + at] : 0.0f;
-        }
+        for (int r = 0; r < RT; ++r) gv[u][r] = p.g[(int64_t)t * h_row + min(r0 + r * 16 + row, rank - 1)];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool mine = id[u] == l;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) xv[u][d] = mine ? xv[u][d] : 0u;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) gv[u][r] = mine && r0 + r * 16 + row < rank ? gv[u][r] : 0.0f;
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
@@ -554,6 +581,14 @@ hipError_t run_shrink(const Shrink& p0, const Shrink& p1, int products, const Lo
   return hipGetLastError();
 }
 
+template <typename T, int STEPS>
+void run_expand_as(const Expand& p, const LowrankArgs& a, dim3 grid, int run, int across, hipStream_t s) {
+  if ((int64_t)a.tokens * p.outputs * (int)sizeof(T) >= kStreamBytes)
+    expand_tile<T, STEPS, true><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
+  else
+    expand_tile<T, STEPS, false><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
+}
+
 template <typename T>
 hipError_t run_expand(const Expand& p, const LowrankArgs& a, hipStream_t s) {
   // runs of tokens: some 2048 workgroups, a run not under 16 tokens
@@ -562,11 +597,10 @@ hipError_t run_expand(const Expand& p, const LowrankArgs& a, hipStream_t s) {
   run = (run + 15) / 16 * 16;
   const dim3 grid((unsigned)((a.tokens + run - 1) / run * across));
   const int steps = (a.rank + 4 * kVec<T> - 1) / (4 * kVec<T>);
-  if (steps <= 1) expand_tile<T, 1><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
-  else if (steps <= 2) expand_tile<T, 2><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
-  else if (steps <= 4) expand_tile<T, 4><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
-  else if constexpr (sizeof(T) == 4)
-    expand_tile<T, 8><<<grid, 256, 0, s>>>(p, a.ids, a.tokens, a.rank, a.adapters, run, across);
+  if (steps <= 1) run_expand_as<T, 1>(p, a, grid, run, across, s);
+  else if (steps <= 2) run_expand_as<T, 2>(p, a, grid, run, across, s);
+  else if (steps <= 4) run_expand_as<T, 4>(p, a, grid, run, across, s);
+  else if constexpr (sizeof(T) == 4) run_expand_as<T, 8>(p, a, grid, run, across, s);
   return hipGetLastError();
 }
 

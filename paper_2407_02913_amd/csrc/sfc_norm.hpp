@@ -42,6 +42,7 @@ struct NormArgs {
   FastDiv by_vps, by_p;    // vector -> run; planes: element of a group -> channel; channels last: channel -> group
   int threads, per_thread; // resident kernels: of a workgroup, and vectors of a thread (0: two kernels)
   int finals;              // workgroups in front that add up part_c
+  bool stream;             // the result is stored past the caches
 };
 
 // y = act(z)
@@ -141,11 +142,10 @@ __device__ __forceinline__ void store_i8(int8_t* p, const float (&v)[V], float i
 }
 
 template <typename TO, int V>
-__device__ __forceinline__ void store_out(TO* p, const float (&v)[V], float inv, int valid) {
-  if constexpr (__is_same(TO, int8_t))
-    store_i8<V>(p, v, inv, valid);
-  else
-    store_vec<TO, V>(p, v, valid);
+__device__ __forceinline__ void store_out(const NormArgs& a, TO* p, const float (&v)[V], int valid) {
+  if constexpr (__is_same(TO, int8_t)) store_i8<V>(p, v, a.inv_y, valid);
+  else if (a.stream) store_vec<TO, V, true>(p, v, valid);
+  else store_vec<TO, V>(p, v, valid);
 }
 
 // Sum of one value a thread over a workgroup, in every thread; `scratch` holds a float per wave and is free
@@ -164,14 +164,28 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
 // the mean of means, then squares about it, so nothing large is subtracted.
 __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g, int lane, int width) {
   const float4* part = reinterpret_cast<const float4*>(a.part) + ((int64_t)n * a.G + g) * a.chunks;
+  constexpr int KEPT = 4;  // parts of a lane that need no second read
+  float4 kept[KEPT];
   float sum = 0.0f, squares = 0.0f;
-  for (int i = lane; i < a.chunks; i += width) {
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k) {
+    const int i = lane + k * width;
+    kept[k] = i < a.chunks ? part[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  }
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k) sum = fmaf(kept[k].x, kept[k].z, sum);
+  for (int i = lane + KEPT * width; i < a.chunks; i += width) {
     const float4 p = part[i];
     sum = fmaf(p.x, p.z, sum);
   }
   for (int m = width >> 1; m; m >>= 1) sum += __shfl_xor(sum, m, 64);
   const float inv = 1.0f / ((float)a.cpg * (float)a.P), mean = sum * inv;
-  for (int i = lane; i < a.chunks; i += width) {
+#pragma unroll
+  for (int k = 0; k < KEPT; ++k) {
+    const float d = kept[k].x - mean;
+    squares += lane + k * width < a.chunks ? fmaf(d * d, kept[k].z, kept[k].y) : 0.0f;
+  }
+  for (int i = lane + KEPT * width; i < a.chunks; i += width) {
     const float4 p = part[i];
     const float d = p.x - mean;
     squares += fmaf(d * d, p.z, p.y);

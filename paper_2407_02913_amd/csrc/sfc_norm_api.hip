@@ -57,6 +57,7 @@ sfc_status describe(const sfc_group_norm_desc* d, NormArgs* a, bool* nothing) {
   a->activation = d->activation;
   a->eps = d->eps;
   a->inv_y = i8 ? 1.0f / d->y_scale : 0.0f;
+  a->stream = (int64_t)d->N * d->C * pixels * type_size(d->y_type) >= sfc::kStreamBytes;
   *nothing = d->N == 0 || pixels == 0;
   return SFC_OK;
 }

@@ -13,6 +13,10 @@
 namespace sfc {
 namespace {
 
+// Most threads of the kernels in two steps: as many vector columns as the widest group has.
+template <typename T>
+constexpr int kMost = 4096 / kVec<T>;
+
 // A thread's place in its workgroup's slab.
 template <typename T>
 struct Column {
@@ -30,6 +34,33 @@ struct Column {
     rows = (int)blockDim.x >> a.lanes;
     c = g0 * a.cpg + col * kVec<T>;
     valid = max(0, min(kVec<T>, width - col * kVec<T>));
+  }
+};
+
+// A column's vector of the pixel at `p`: WHOLE, no vector of the slab is cut short.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ raw4 load_column(const T* p, const Column<T>& k, int64_t room) {
+  if constexpr (WHOLE) return load16(p);
+  return load_cut(p, k.valid, room);
+}
+
+// z of one vector from the group's statistics: (x - mean) / sd first, so that a mean far from zero costs nothing of
+// float32's digits; 16-bit values do not have the digits it would cost, and take one instruction.
+template <typename T>
+struct Affine {
+  static constexpr bool kFolded = sizeof(T) == 2;
+  float w[kVec<T>], b[kVec<T>], mean[kFolded ? 1 : kVec<T>], rstd[kFolded ? 1 : kVec<T>];
+  __device__ __forceinline__ void set(int j, float weight, float bias, float2 stat) {
+    if constexpr (kFolded) {
+      w[j] = stat.y * weight;
+      b[j] = fmaf(-stat.x, w[j], bias);
+    } else {
+      w[j] = weight, b[j] = bias, mean[j] = stat.x, rstd[j] = stat.y;
+    }
+  }
+  __device__ __forceinline__ float operator()(int j, float x) const {
+    if constexpr (kFolded) return fmaf(x, w[j], b[j]);
+    return fmaf((x - mean[kFolded ? 0 : j]) * rstd[kFolded ? 0 : j], w[j], b[j]);
   }
 };
 
@@ -152,16 +183,15 @@ __global__ __launch_bounds__(1024) void last_resident(NormArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j) z[j] = fmaf((element<TI>(raw[u], j) - mean[j]) * rstd[j], w[j], b[j]);
       activate<V>(a.activation, z);
-      store_out<TO, V>(y + p * a.ys_r, z, a.inv_y, k.valid);
+      store_out<TO, V>(a, y + p * a.ys_r, z, k.valid);
     }
   }
 }
 
-// Sums of a part of the pixels.  A channel's mean and squares about it are carried along in each thread
-// (m += d / i, s += d d'), so that a mean far from zero costs no digits; the threads' are joined about the
-// group's mean.
-template <typename TI>
-__global__ __launch_bounds__(1024) void last_stats(NormArgs a) {
+// Sums of a part of the pixels.  Each thread adds a channel's values and squares about its first one, so that a mean far
+// from zero costs no digits; the threads' means and squares are joined about the group's mean.
+template <typename TI, bool WHOLE>
+__global__ __launch_bounds__(kMost<TI>) void last_stats(NormArgs a) {
   constexpr int V = kVec<TI>;
   extern __shared__ float4 lds[];
   const int id = blockIdx.x / a.chunks, chunk = blockIdx.x - id * a.chunks, n = id / a.slabs;
@@ -169,30 +199,44 @@ __global__ __launch_bounds__(1024) void last_stats(NormArgs a) {
   const int first = chunk * a.per, last = min(a.P, first + a.per);
   const TI* x = static_cast<const TI*>(a.x) + n * a.xs_n + k.c;
   const int64_t room = a.x_end - n * a.xs_n - k.c;
-  float m[V], s[V];
+  float about[V], m[V], s[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) m[j] = s[j] = 0.0f;
-  int count = 0;
-  if (k.valid) {
-    for (int p = first + k.row; p < last; p += 4 * k.rows) {
+  for (int j = 0; j < V; ++j) about[j] = m[j] = s[j] = 0.0f;
+  // (pixels first + row, + rows, ...: `count` of them)
+  const int mine = last - first - k.row;
+  const int count = k.valid && mine > 0 ? (mine + k.rows - 1) / k.rows : 0;
+  if (count) {
+    const int64_t step = k.rows * a.xs_r;
+    int64_t at = (first + k.row) * a.xs_r;
+    auto load = [&](int u) { return load_column<TI, WHOLE>(x + at + u * step, k, room - at - u * step); };
+    auto add = [&](const raw4& r) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float d = element<TI>(r, j) - about[j];
+        m[j] += d;
+        s[j] = fmaf(d, d, s[j]);
+      }
+    };
+    int i = 0;
+    {
+      const raw4 r = load(0);
+#pragma unroll
+      for (int j = 0; j < V; ++j) about[j] = element<TI>(r, j);
+    }
+    for (; i + 4 <= count; i += 4, at += 4 * step) {
       raw4 r[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int q = p + u * k.rows;
-        if (q < last) r[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
-      }
+      for (int u = 0; u < 4; ++u) r[u] = load(u);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (p + u * k.rows < last) {
-          const float step = __builtin_amdgcn_rcpf((float)++count);
+      for (int u = 0; u < 4; ++u) add(r[u]);
+    }
+    for (; i < count; ++i, at += step) add(load(0));
+    const float inv = 1.0f / (float)count;
 #pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const float e = element<TI>(r[u], j), d = e - m[j];
-            m[j] = fmaf(d, step, m[j]);
-            s[j] = fmaf(d, e - m[j], s[j]);
-          }
-        }
-      }
+    for (int j = 0; j < V; ++j) {
+      const float d = m[j] * inv;
+      s[j] = fmaxf(fmaf(-m[j], d, s[j]), 0.0f * s[j]);  // (not below zero; a NaN stays one)
+      m[j] = about[j] + d;
     }
   }
   int group[V];
@@ -226,8 +270,8 @@ __device__ __forceinline__ void slab_stats(const NormArgs& a, int n, int g0, int
   __syncthreads();
 }
 
-template <typename TI, typename TO>
-__global__ __launch_bounds__(1024) void last_apply(NormArgs a) {
+template <typename TI, typename TO, bool WHOLE>
+__global__ __launch_bounds__(kMost<TI>) void last_apply(NormArgs a) {
   constexpr int V = kVec<TI>;
   extern __shared__ float4 lds[];
   float2* stat = reinterpret_cast<float2*>(lds);
@@ -241,32 +285,37 @@ __global__ __launch_bounds__(1024) void last_apply(NormArgs a) {
   if (chunk == 0)
     for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
       reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] = stat[g];
-  if (!k.valid) return;
-  float w[V], b[V], mean[V], rstd[V];
-  int group[V];
-  affine_of<TI>(a, k, w, b);
-  groups_of<TI>(a, k, group);
+  const int mine = last - first - k.row;
+  const int count = k.valid && mine > 0 ? (mine + k.rows - 1) / k.rows : 0;
+  if (!count) return;
+  Affine<TI> affine;
+  {
+    float w[V], b[V];
+    int group[V];
+    affine_of<TI>(a, k, w, b);
+    groups_of<TI>(a, k, group);
 #pragma unroll
-  for (int j = 0; j < V; ++j) mean[j] = stat[group[j]].x, rstd[j] = stat[group[j]].y;
-  for (int p = first + k.row; p < last; p += 4 * k.rows) {
+    for (int j = 0; j < V; ++j) affine.set(j, w[j], b[j], stat[group[j]]);
+  }
+  const int64_t step = k.rows * a.xs_r, step_y = k.rows * a.ys_r;
+  int64_t at = (first + k.row) * a.xs_r, to = (first + k.row) * a.ys_r;
+  auto load = [&](int u) { return load_column<TI, WHOLE>(x + at + u * step, k, room - at - u * step); };
+  auto store = [&](int u, const raw4& r) {
+    float z[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) z[j] = affine(j, element<TI>(r, j));
+    activate<V>(a.activation, z);
+    store_out<TO, V>(a, y + to + u * step_y, z, WHOLE ? V : k.valid);
+  };
+  int i = 0;
+  for (; i + 4 <= count; i += 4, at += 4 * step, to += 4 * step_y) {
     raw4 r[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int q = p + u * k.rows;
-      if (q < last) r[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
-    }
+    for (int u = 0; u < 4; ++u) r[u] = load(u);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int q = p + u * k.rows;
-      if (q < last) {
-        float z[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) z[j] = fmaf((element<TI>(r[u], j) - mean[j]) * rstd[j], w[j], b[j]);
-        activate<V>(a.activation, z);
-        store_out<TO, V>(y + q * a.ys_r, z, a.inv_y, k.valid);
-      }
-    }
+    for (int u = 0; u < 4; ++u) store(u, r[u]);
   }
+  for (; i < count; ++i, at += step, to += step_y) store(0, load(0));
 }
 
 // ---- backward ----
@@ -290,7 +339,7 @@ __device__ __forceinline__ void back_vector(const NormArgs& a, const raw4& x, co
 
 // Sums of a part of the pixels: of each channel (part_c: dz, dz h) and of each group (part: w dz, w dz h).
 template <typename T>
-__global__ __launch_bounds__(1024) void last_back_sums(NormArgs a) {
+__global__ __launch_bounds__(kMost<T>) void last_back_sums(NormArgs a) {
   constexpr int V = kVec<T>;
   extern __shared__ float4 lds[];
   const int id = blockIdx.x / a.chunks, chunk = blockIdx.x - id * a.chunks, n = id / a.slabs;
@@ -369,7 +418,7 @@ __global__ __launch_bounds__(1024) void last_back_sums(NormArgs a) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store_dx(const float (&rstd)[kVec<T>], const float (&w)[kVec<T>],
+__device__ __forceinline__ void store_dx(const NormArgs& a, const float (&rstd)[kVec<T>], const float (&w)[kVec<T>],
                                          const float (&c1)[kVec<T>], const float (&c2)[kVec<T>],
                                          const float (&h)[kVec<T>], const float (&dz)[kVec<T>], T* dx, int valid) {
 // (the product is rounded before the difference, as in the sums: a group of one element gives exactly zero)
@@ -381,11 +430,11 @@ __device__ __forceinline__ void store_dx(const float (&rstd)[kVec<T>], const flo
     const float d = dz[j] * w[j] - c1[j];
     v[j] = rstd[j] * (d - h[j] * c2[j]);
   }
-  store_vec<T, V>(dx, v, valid);
+  store_out<T, V>(a, dx, v, valid);
 }
 
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void last_back_apply(NormArgs a) {
+template <typename T>
+__global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   constexpr int V = kVec<T>;
   extern __shared__ float4 lds[];
   if ((int)blockIdx.x < a.finals) {
@@ -438,7 +487,7 @@ __global__ __launch_bounds__(THREADS) void last_back_apply(NormArgs a) {
       if (q < last) {
         float h[V], dz[V];
         back_vector<T>(a, rx[u], ry[u], mean, rstd, w, b, h, dz);
-        store_dx<T>(rstd, w, c1, c2, h, dz, dx + q * a.xs_r, k.valid);
+        store_dx<T>(a, rstd, w, c1, c2, h, dz, dx + q * a.xs_r, k.valid);
       }
     }
   }
@@ -457,16 +506,17 @@ void set_slab(NormArgs* a, int groups, int V) {
   a->by_p = FastDiv::by((unsigned)a->cpg);  // channel of the slab -> group
 }
 
-// Two kernels: as many whole groups as 256 threads have vector columns for (a wider group has 1024), and parts
-// of the pixels for some 2048 workgroups, each of at least 4 rows of threads; the parts of one image stay few enough
-// for every workgroup of the second kernel to join them (4096 group parts: 64 KB out of the L2).
+// Two kernels: as many whole groups as 256 threads have vector columns for (a wider group: more), and parts of the pixels
+// for some 1024 workgroups, each of at least 4 rows of threads.  Every workgroup of the second kernel joins the parts of
+// its image: where the maps are large, workgroups of 512 threads halve their number, and they stay below 4096 (64 KB).
 void set_parts(NormArgs* a, int x_size) {
   const int V = 16 / x_size;
-  a->threads = a->cpg > 256 * V ? 1024 : 256;
+  const bool large = (int64_t)a->N * a->P * a->C >= ((int64_t)1 << 24);
+  a->threads = a->cpg > 512 * V ? 1024 : a->cpg > 256 * V || large ? 512 : 256;
   set_slab(a, a->cpg < 256 * V ? 256 * V / a->cpg : 1, V);
   const int rows = a->threads >> a->lanes;
   const int64_t cells = (int64_t)a->N * a->slabs;
-  int64_t parts = (2048 + cells - 1) / cells;
+  int64_t parts = ((large ? 1024 : 2048) + cells - 1) / cells;
   const int64_t most = a->P / (4 * rows) > 1 ? a->P / (4 * rows) : 1;
   parts = parts < most ? parts : most;
   const int64_t joined = 4096 / a->slab > 1 ? 4096 / a->slab : 1;
@@ -516,6 +566,20 @@ size_t plan_norm_last_backward(NormArgs* a, int x_size) {
 
 namespace {
 
+// Whether no slab cuts a vector (the last slab's groups may be fewer).
+template <typename T>
+bool whole_vectors(const NormArgs& a) {
+  return a.slab * a.cpg % kVec<T> == 0 && a.C % kVec<T> == 0;
+}
+
+template <typename T>
+void run_stats(const NormArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.N * a.slabs * a.chunks)), block((unsigned)a.threads);
+  const unsigned bytes = sums_bytes(a, kVec<T>);
+  if (whole_vectors<T>(a)) last_stats<T, true><<<grid, block, bytes, s>>>(a);
+  else last_stats<T, false><<<grid, block, bytes, s>>>(a);
+}
+
 template <typename TI, typename TO>
 hipError_t run_last(const NormArgs& a, hipStream_t s) {
   constexpr int V = kVec<TI>;
@@ -531,8 +595,9 @@ hipError_t run_last(const NormArgs& a, hipStream_t s) {
     return hipGetLastError();
   }
   const dim3 grid((unsigned)((int64_t)a.N * a.slabs * a.chunks)), block((unsigned)a.threads);
-  last_stats<TI><<<grid, block, sums_bytes(a, V), s>>>(a);
-  last_apply<TI, TO><<<grid, block, (unsigned)a.slab * 8u, s>>>(a);
+  run_stats<TI>(a, s);
+  if (whole_vectors<TI>(a)) last_apply<TI, TO, true><<<grid, block, (unsigned)a.slab * 8u, s>>>(a);
+  else last_apply<TI, TO, false><<<grid, block, (unsigned)a.slab * 8u, s>>>(a);
   return hipGetLastError();
 }
 
@@ -545,9 +610,7 @@ hipError_t run_last_back(NormArgs a, hipStream_t s) {
   a.finals = a.dweight || a.dbias ? (a.C + 7) / 8 : 0;
   const unsigned bytes = (unsigned)a.slab * 8u;
   const dim3 grid(cells + (unsigned)a.finals);
-  // (registers for 256 threads where the slab allows it: with the 128 of a larger workgroup some would spill)
-  if (a.threads == 256) last_back_apply<T, 256><<<grid, block, bytes > 256u ? bytes : 256u, s>>>(a);
-  else last_back_apply<T, 1024><<<grid, block, bytes > 1024u ? bytes : 1024u, s>>>(a);
+  last_back_apply<T><<<grid, block, bytes > 1024u ? bytes : 1024u, s>>>(a);
   return hipGetLastError();
 }
 
@@ -563,10 +626,9 @@ hipError_t launch_norm_last(const NormArgs& a, int x_type, int y_type, hipStream
 }
 
 hipError_t launch_norm_last_stats(const NormArgs& a, int x_type, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.N * a.slabs * a.chunks)), block((unsigned)a.threads);
-  if (x_type == kNormF32) last_stats<float><<<grid, block, sums_bytes(a, 4), s>>>(a);
-  else if (x_type == kNormF16) last_stats<f16><<<grid, block, sums_bytes(a, 8), s>>>(a);
-  else last_stats<bf16><<<grid, block, sums_bytes(a, 8), s>>>(a);
+  if (x_type == kNormF32) run_stats<float>(a, s);
+  else if (x_type == kNormF16) run_stats<f16>(a, s);
+  else run_stats<bf16>(a, s);
   return hipGetLastError();
 }
 

@@ -59,7 +59,7 @@ __device__ __forceinline__ void finish_item(const NormArgs& a, const Item& it, c
     z[j] = fmaf((element<TI>(raw, j) - stat.x) * stat.y, w.x, w.y);
   }
   activate<V>(a.activation, z);
-  store_out<TO, V>(y, z, a.inv_y, it.valid);
+  store_out<TO, V>(a, y, z, it.valid);
 }
 
 template <typename TI, typename TO, int NV>
@@ -225,7 +225,7 @@ __device__ __forceinline__ void back_item(const NormArgs& a, const Item& it, con
 // dx = rstd (w dz - c1 - h c2), c1 and c2 the group's means of w dz and w dz h.  The product is rounded before the
 // difference, as in the sums: a group of one element then gives exactly zero.
 template <typename T>
-__device__ __forceinline__ void store_dx(const Item& it, float2 stat, float c1, float c2, const float2* wb,
+__device__ __forceinline__ void store_dx(const NormArgs& a, const Item& it, float2 stat, float c1, float c2, const float2* wb,
                                          const float (&h)[kVec<T>], const float (&dz)[kVec<T>], T* dx) {
 #pragma clang fp contract(off)
   constexpr int V = kVec<T>;
@@ -236,7 +236,7 @@ __device__ __forceinline__ void store_dx(const Item& it, float2 stat, float c1, 
     const float d = dz[j] * (j < it.bound ? w0 : w1) - c1;
     v[j] = stat.y * (d - h[j] * c2);
   }
-  store_vec<T, V>(dx, v, it.valid);
+  store_out<T, V>(a, dx, v, it.valid);
 }
 
 // Sums of a vector's two channels: (dz, dz h) of ch in `head`, of ch + 1 in `next`.
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(1024) void planes_back_resident(NormArgs a) {
       const Item it = item_of<T>(a, q, a.xs_r);
       float h[kVec<T>], dz[kVec<T>];
       back_item<T>(a, it, rx[u], ry[u], stat, wb, h, dz);
-      store_dx<T>(it, stat, c1, c2, wb, h, dz, dx + it.at);
+      store_dx<T>(a, it, stat, c1, c2, wb, h, dz, dx + it.at);
     }
   }
 }
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(256) void planes_back_apply(NormArgs a) {
       if (q + 256 * k < last) {
         float h[kVec<T>], dz[kVec<T>];
         back_item<T>(a, it[k], rx[k], ry[k], stat, lds, h, dz);
-        store_dx<T>(it[k], stat, c1, c2, lds, h, dz, dx + it[k].at);
+        store_dx<T>(a, it[k], stat, c1, c2, lds, h, dz, dx + it[k].at);
       }
     }
   }

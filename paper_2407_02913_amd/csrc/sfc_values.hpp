@@ -74,8 +74,8 @@ __device__ __forceinline__ float element(const raw4& r, int j) {
   }
 }
 
-// Floats rounded to nearest even, as T, in the dwords that are stored.
-template <typename T, int V>
+// Floats rounded to nearest even, as T, in the dwords that are stored.  STREAM: past the caches (kStreamBytes).
+template <typename T, int V, bool STREAM = false>
 __device__ __forceinline__ void store_vec(T* p, const float (&v)[V], int valid) {
   typedef T pack __attribute__((ext_vector_type(V)));
   if constexpr (sizeof(T) * V == 16 || sizeof(T) * V == 8 || sizeof(T) * V == 4) {
@@ -84,7 +84,14 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[V], int valid) 
 #pragma unroll
       for (int j = 0; j < V; ++j) o[j] = (T)v[j];
       typedef T loose __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-      *reinterpret_cast<loose*>(p) = o;
+      if constexpr (STREAM) {
+        // (fenced in: where both stores are arms of one branch they would be made one, which is not streamed)
+        asm volatile("");
+        __builtin_nontemporal_store(o, reinterpret_cast<loose*>(p));
+        asm volatile("");
+      } else {
+        *reinterpret_cast<loose*>(p) = o;
+      }
       return;
     }
   }
@@ -92,6 +99,11 @@ __device__ __forceinline__ void store_vec(T* p, const float (&v)[V], int valid) 
   for (int j = 0; j < V; ++j)
     if (j < valid) p[j] = (T)v[j];
 }
+
+// Results of this many bytes and more, twice the L2 caches, are stored past them: what the next kernel reads first would
+// wait for them to be written back (group norm, channels last, 32 224x224 maps of 64 channels in bfloat16: the two
+// kernels 134 us, 116 stored so).  Smaller ones stay where their reader finds them.
+constexpr int64_t kStreamBytes = (int64_t)64 << 20;
 
 // Sum over the lanes of a wave whose numbers agree modulo `group` (a power of two below 64; 1: all lanes),
 // in every one of them.
