@@ -20,7 +20,13 @@
 namespace sfc {
 namespace {
 
+// Up to this many tokens go one by one.  4096 inputs and outputs, rank 16, bfloat16, 256 tokens with an adapter each: 12 us,
+// all with one adapter 9; as tiles, at 512 tokens, 78 and 10.
 constexpr int kFew = 256;
+// A token in one kernel up to this many bytes of its adapter's factors, else in two that spread them over the chip: with
+// 256 KB 8.1 us against 6.4 at 64 tokens and 12 against 15 at 256, one launch instead of two; with 1 MB 28 against 7 for a
+// single token.
+constexpr int kWholeBytes = 256 << 10;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -74,6 +80,81 @@ __device__ __forceinline__ raw4 to_operand(const raw4& v) {
 }
 
 // ---- few tokens ----
+
+// A token to a workgroup of sixteen waves, both products in one kernel: a wave adds up a rank at a time, a thread an
+// output.  What the second product reads of the bank first is asked for ahead of the first product.
+template <typename T>
+__global__ __launch_bounds__(1024) void token_whole(const T* x, int64_t x_stride, const int32_t* ids, const T* down,
+                                                    const T* up, const float* scale, const T* base, int64_t base_stride,
+                                                    T* y, int64_t y_stride, int tokens, int inputs, int outputs, int rank,
+                                                    int adapters) {
+  constexpr int V = kVec<T>, AHEAD = 16 / V;  // vectors of a row of `up` that are asked for ahead: 16 ranks
+  __shared__ float h[128];
+  const int t = blockIdx.x, l = ids[t], lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (l < 0 || l >= adapters) {
+    for (int m = threadIdx.x; m < outputs; m += 1024)
+      y[t * y_stride + m] = base ? base[t * base_stride + m] : (T)0.0f;
+    return;
+  }
+  const int64_t of_up = (int64_t)l * outputs * rank, room_up = (int64_t)adapters * outputs * rank - of_up;
+  const T* u_row = up + of_up;
+  auto ahead = [&](int m, raw4 (&w)[AHEAD], float* b) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      w[i] = raw4{0u, 0u, 0u, 0u};
+      const int64_t at = (int64_t)m * rank + i * V;
+      if (m < outputs && i * V < rank) w[i] = load_cut(u_row + at, rank - i * V, room_up - at);
+    }
+    *b = base && m < outputs ? (float)base[t * base_stride + m] : 0.0f;
+  };
+  raw4 w[AHEAD];
+  float b;
+  ahead(threadIdx.x, w, &b);
+  const T* row = x + t * x_stride;
+  const int64_t room_x = (tokens - 1 - t) * x_stride + inputs;
+  for (int r = wave; r < rank; r += 16) {
+    const int64_t at = ((int64_t)l * rank + r) * inputs, room = (int64_t)adapters * rank * inputs - at;
+    const T* d = down + at;
+    float s = 0.0f;
+    for (int k0 = lane * V; k0 < inputs; k0 += 4 * 64 * V) {
+      raw4 p[4], q[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int k = k0 + u * 64 * V;
+        p[u] = q[u] = raw4{0u, 0u, 0u, 0u};
+        if (k < inputs) p[u] = load_cut(row + k, inputs - k, room_x - k), q[u] = load_cut(d + k, inputs - k, room - k);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int j = 0; j < V; ++j) s = fmaf(element<T>(p[u], j), element<T>(q[u], j), s);
+    }
+    s = wave_sum(s);
+    if (lane == 0) h[r] = s;
+  }
+  __syncthreads();
+  const float f = scale ? scale[l] : 1.0f;
+  for (int m = threadIdx.x; m < outputs; m += 1024) {
+    raw4 next[AHEAD];
+    float next_b = 0.0f;
+    ahead(m + 1024, next, &next_b);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+      for (int j = 0; j < V; ++j) s = fmaf(element<T>(w[i], j), i * V + j < rank ? h[i * V + j] : 0.0f, s);
+    for (int r = 16; r < rank; r += V) {
+      const int64_t at = (int64_t)m * rank + r;
+      const raw4 v = load_cut(u_row + at, rank - r, room_up - at);
+#pragma unroll
+      for (int j = 0; j < V; ++j) s = fmaf(element<T>(v, j), r + j < rank ? h[r + j] : 0.0f, s);
+    }
+    y[t * y_stride + m] = (T)fmaf(f, s, b);
+    b = next_b;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) w[i] = next[i];
+  }
+}
 
 template <typename T>
 __global__ __launch_bounds__(256) void shrink_few(const T* x, int64_t x_stride, const int32_t* ids, const T* down, float* h,
@@ -614,6 +695,13 @@ Shrink shrink_of(const void* x, const void* bank, void* h, int64_t stride, int i
 template <typename T>
 hipError_t run_lowrank(const LowrankArgs& a, hipStream_t s) {
   float* h = reinterpret_cast<float*>(a.space);
+  if (a.tokens <= kFew && (int64_t)a.rank * (a.inputs + a.outputs) * (int)sizeof(T) <= kWholeBytes) {
+    token_whole<T><<<dim3((unsigned)a.tokens), 1024, 0, s>>>(
+        static_cast<const T*>(a.x), a.x_stride, a.ids, static_cast<const T*>(a.down), static_cast<const T*>(a.up), a.scale,
+        static_cast<const T*>(a.base), a.base_stride, static_cast<T*>(a.y), a.y_stride, a.tokens, a.inputs, a.outputs,
+        a.rank, a.adapters);
+    return hipGetLastError();
+  }
   if (a.tokens <= kFew) {
     shrink_few<T><<<dim3((unsigned)a.tokens, (unsigned)(a.rank + 3) / 4u), 256, 0, s>>>(
         static_cast<const T*>(a.x), a.x_stride, a.ids, static_cast<const T*>(a.down), h, a.tokens, a.inputs, a.rank,
