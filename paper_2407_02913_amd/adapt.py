@@ -266,7 +266,12 @@ def add_adapters(base, x, ids, down, up, scale=None, out=None):
     outputs, device = fields[2], x.device
     plan = _lowrank(*fields, _row_stride(x, "x"), _check_rows("base", base, x, outputs),
                     _check_rows("out", out, x, outputs), 0)
-    y = torch.empty((fields[0], outputs), dtype=x.dtype, device=device) if out is None else out
+    if out is not None:
+        y = out
+    elif base is not None and base.is_contiguous():
+        y = torch.empty_like(base)
+    else:
+        y = torch.empty((fields[0], outputs), dtype=x.dtype, device=device)
     space = _bytes(plan.forward_bytes, device)
     _call(device, "sfc_lowrank_add", plan.at, x.data_ptr(), ids.data_ptr(), down.data_ptr(), up.data_ptr(), _ptr(scale),
           _ptr(base), y.data_ptr(), _ptr(space), plan.forward_bytes)

@@ -219,13 +219,13 @@ struct Shrink {
   int inputs;
 };
 
-// h of 16 TT tokens: waves share the inputs in turns of 128 bytes a row, and add up in LDS.  RT: sixteens of the rank.
+// h of 16 TT tokens: waves share the inputs in turns of 64 U bytes a row, and add up in LDS.  RT: sixteens of the rank.
 // Tiles begin at different inputs: rows are a power of two apart more often than not, and tiles that read the same
 // columns at the same time would keep to a part of the memory's channels.
-template <typename T, int RT, int TT, int WAVES>
+template <typename T, int RT, int TT, int WAVES, int U>
 __global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, const int32_t* ids, const float* scale,
                                                           int2* range, int tokens, int rank, int adapters) {
-  constexpr int V = kVec<T>, STEP = 4 * V, CHUNK = 2 * STEP, TOKENS = 16 * TT;
+  constexpr int V = kVec<T>, STEP = 4 * V, CHUNK = U * STEP, TOKENS = 16 * TT;
   constexpr uint64_t ALL = (1ull << TOKENS) - 1;
   __shared__ v4f sums[WAVES][RT][TT][64];
   const Shrink p = blockIdx.y ? p1 : p0;
@@ -259,16 +259,16 @@ __global__ __launch_bounds__(WAVES * 64) void shrink_tile(Shrink p0, Shrink p1, 
       for (int i = 0; i < TT; ++i) acc[r][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     for (int c = wave; c < chunks; c += WAVES) {
       const int from = c + turn, k = (from < chunks ? from : from - chunks) * CHUNK;
-      raw4 a[2][TT], b[2][RT];
+      raw4 a[U][TT], b[U][RT];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int i = 0; i < TT; ++i) a[u][i] = load16(x + at_x[i] + k + u * STEP);
 #pragma unroll
         for (int r = 0; r < RT; ++r) b[u][r] = load16(w + at_w[r] + k + u * STEP);
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int i = 0; i < TT; ++i) a[u][i] = to_operand(a[u][i]);
 #pragma unroll
@@ -634,30 +634,34 @@ __global__ __launch_bounds__(256) void outer_finish(const float* part_down, cons
   }
 }
 
+bool token_is_whole(const LowrankArgs& a, int size) {
+  return a.tokens <= kFew && (int64_t)a.rank * (a.inputs + a.outputs) * size <= kWholeBytes;
+}
+
 size_t up64(size_t v) { return (v + 63) / 64 * 64; }
 
-template <typename T, int RT, int TT, int WAVES>
+template <typename T, int RT, int TT, int WAVES, int U>
 void run_shrink_as(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
   const dim3 grid((unsigned)((a.tokens + 16 * TT - 1) / (16 * TT)), (unsigned)products);
-  shrink_tile<T, RT, TT, WAVES><<<grid, WAVES * 64, 0, s>>>(p0, p1, a.ids, a.scale, range, a.tokens, a.rank, a.adapters);
+  shrink_tile<T, RT, TT, WAVES, U><<<grid, WAVES * 64, 0, s>>>(p0, p1, a.ids, a.scale, range, a.tokens, a.rank, a.adapters);
 }
 
 template <typename T>
 hipError_t run_shrink(const Shrink& p0, const Shrink& p1, int products, const LowrankArgs& a, int2* range, hipStream_t s) {
-  // (tiles of 16 tokens where 32 would leave compute units without a workgroup)
+  // (tiles of 16 tokens, more waves and longer turns where 32 would leave compute units without a workgroup)
   const bool small = (int64_t)products * a.tokens < 32 * 512;
   if (a.rank <= 16) {
-    if (small) run_shrink_as<T, 1, 1, 8>(p0, p1, products, a, range, s);
-    else run_shrink_as<T, 1, 2, 8>(p0, p1, products, a, range, s);
+    if (small) run_shrink_as<T, 1, 1, 8, 4>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 1, 2, 8, 4>(p0, p1, products, a, range, s);
   } else if (a.rank <= 32) {
-    if (small) run_shrink_as<T, 2, 1, 8>(p0, p1, products, a, range, s);
-    else run_shrink_as<T, 2, 2, 8>(p0, p1, products, a, range, s);
+    if (small) run_shrink_as<T, 2, 1, 16, 2>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 2, 2, 8, 4>(p0, p1, products, a, range, s);
   } else if (a.rank <= 64) {
-    if (small) run_shrink_as<T, 4, 1, 8>(p0, p1, products, a, range, s);
-    else run_shrink_as<T, 4, 2, 4>(p0, p1, products, a, range, s);
+    if (small) run_shrink_as<T, 4, 1, 8, 2>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 4, 2, 4, 2>(p0, p1, products, a, range, s);
   } else {
-    if (small) run_shrink_as<T, 8, 1, 4>(p0, p1, products, a, range, s);
-    else run_shrink_as<T, 8, 2, 4>(p0, p1, products, a, range, s);
+    if (small) run_shrink_as<T, 8, 1, 4, 2>(p0, p1, products, a, range, s);
+    else run_shrink_as<T, 8, 2, 4, 2>(p0, p1, products, a, range, s);
   }
   return hipGetLastError();
 }
@@ -695,7 +699,7 @@ Shrink shrink_of(const void* x, const void* bank, void* h, int64_t stride, int i
 template <typename T>
 hipError_t run_lowrank(const LowrankArgs& a, hipStream_t s) {
   float* h = reinterpret_cast<float*>(a.space);
-  if (a.tokens <= kFew && (int64_t)a.rank * (a.inputs + a.outputs) * (int)sizeof(T) <= kWholeBytes) {
+  if (token_is_whole(a, (int)sizeof(T))) {
     token_whole<T><<<dim3((unsigned)a.tokens), 1024, 0, s>>>(
         static_cast<const T*>(a.x), a.x_stride, a.ids, static_cast<const T*>(a.down), static_cast<const T*>(a.up), a.scale,
         static_cast<const T*>(a.base), a.base_stride, static_cast<T*>(a.y), a.y_stride, a.tokens, a.inputs, a.outputs,
@@ -806,7 +810,9 @@ hipError_t run_no_tokens(const LowrankArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t lowrank_bytes(const LowrankArgs& a) { return (size_t)a.tokens * row_of(a.rank) * 4; }
+size_t lowrank_bytes(const LowrankArgs& a, int size) {
+  return token_is_whole(a, size) ? 0 : (size_t)a.tokens * row_of(a.rank) * 4;
+}
 
 size_t lowrank_backward_bytes(const LowrankArgs& a, int size) { return plan_backward(a, size).bytes; }
 

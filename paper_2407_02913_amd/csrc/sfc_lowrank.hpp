@@ -20,7 +20,7 @@ struct LowrankArgs {
   int tokens, inputs, outputs, rank, adapters;
 };
 
-size_t lowrank_bytes(const LowrankArgs& a);
+size_t lowrank_bytes(const LowrankArgs& a, int size);
 size_t lowrank_backward_bytes(const LowrankArgs& a, int size);
 // type: sfc_type
 hipError_t launch_lowrank(const LowrankArgs& a, int type, hipStream_t s);

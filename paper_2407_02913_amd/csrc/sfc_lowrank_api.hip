@@ -39,9 +39,9 @@ sfc_status sfc_lowrank_sizes(const sfc_lowrank_desc* desc, size_t* forward_bytes
   LowrankArgs a;
   const sfc_status st = describe(desc, &a);
   if (st != SFC_OK) return st;
-  if (forward_bytes) *forward_bytes = sfc::lowrank_bytes(a);
-  if (backward_bytes)
-    *backward_bytes = a.tokens ? sfc::lowrank_backward_bytes(a, desc->type == SFC_TYPE_F32 ? 4 : 2) : 0;
+  const int size = desc->type == SFC_TYPE_F32 ? 4 : 2;
+  if (forward_bytes) *forward_bytes = sfc::lowrank_bytes(a, size);
+  if (backward_bytes) *backward_bytes = a.tokens ? sfc::lowrank_backward_bytes(a, size) : 0;
   return SFC_OK;
 }
 
@@ -59,7 +59,8 @@ sfc_status sfc_lowrank_add(const sfc_lowrank_desc* desc, const void* x_dev, cons
   if (!aligned(x_dev, size) || !aligned(ids_dev, 4) || !aligned(down_dev, size) || !aligned(up_dev, size) ||
       !aligned(scale_dev, 4) || !aligned(base_dev, size) || !aligned(y_dev, size) || !aligned(workspace_dev, 16))
     return SFC_EINVAL;
-  if (!workspace_dev || workspace_bytes < sfc::lowrank_bytes(a)) return SFC_EWORKSPACE;
+  const size_t need = sfc::lowrank_bytes(a, size);
+  if (need > 0 && (!workspace_dev || workspace_bytes < need)) return SFC_EWORKSPACE;
   a.x = x_dev;
   a.ids = ids_dev;
   a.down = down_dev;

@@ -45,6 +45,11 @@ struct NormArgs {
   bool stream;             // the result is stored past the caches
 };
 
+// 1 / v and 1 / sqrt(v) of the hardware, within a unit of the last place: a wave of a small call waits for every
+// instruction, and the exact ones take some tens.
+__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
+__device__ __forceinline__ float inverse_sqrt(float v) { return __builtin_amdgcn_rsqf(v); }
+
 // y = act(z)
 __device__ __forceinline__ float fast_sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
@@ -179,7 +184,7 @@ __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g,
     sum = fmaf(p.x, p.z, sum);
   }
   for (int m = width >> 1; m; m >>= 1) sum += __shfl_xor(sum, m, 64);
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P), mean = sum * inv;
+  const float inv = inverse((float)a.cpg * (float)a.P), mean = sum * inv;
 #pragma unroll
   for (int k = 0; k < KEPT; ++k) {
     const float d = kept[k].x - mean;
@@ -191,7 +196,7 @@ __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g,
     squares += fmaf(d * d, p.z, p.y);
   }
   for (int m = width >> 1; m; m >>= 1) squares += __shfl_xor(squares, m, 64);
-  return make_float2(mean, 1.0f / sqrtf(fmaf(squares, inv, a.eps)));
+  return make_float2(mean, inverse_sqrt(fmaf(squares, inv, a.eps)));
 }
 
 // Adds part_c over images and parts: workgroup `block` of the `finals` in front, eight channels.

@@ -97,8 +97,10 @@ __device__ __forceinline__ void slab_sums(const NormArgs& a, int groups, float (
   const int width = lanes_of(groups), lane = threadIdx.x & (width - 1);
   for (int g = threadIdx.x / width; g < groups; g += (int)blockDim.x / width) {
     float s = 0.0f;
-    for (int r = 0; r < count; ++r)
-      for (int j = lane; j < a.cpg; j += width) s += rows[r * pitch + g * a.cpg + j];
+    for (int e = lane; e < count * a.cpg; e += width) {
+      const int r = a.by_p(e);
+      s += rows[r * pitch + g * a.cpg + e - r * a.cpg];
+    }
     for (int m = width >> 1; m; m >>= 1) s += __shfl_xor(s, m, 64);
     if (lane == 0) out[g] = s;
   }
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(1024) void last_resident(NormArgs a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] += element<TI>(raw[u], j);
   slab_sums<V>(a, k.groups, v, rows, means);
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float inv = inverse((float)a.cpg * (float)a.P);
   float mean[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) mean[j] = means[group[j]] * inv, v[j] = 0.0f;
@@ -171,10 +173,10 @@ __global__ __launch_bounds__(1024) void last_resident(NormArgs a) {
   slab_sums<V>(a, k.groups, v, rows, rstds);
   float rstd[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) rstd[j] = 1.0f / sqrtf(fmaf(rstds[group[j]], inv, a.eps));
+  for (int j = 0; j < V; ++j) rstd[j] = inverse_sqrt(fmaf(rstds[group[j]], inv, a.eps));
   for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
     reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] =
-        make_float2(means[g] * inv, 1.0f / sqrtf(fmaf(rstds[g], inv, a.eps)));
+        make_float2(means[g] * inv, inverse_sqrt(fmaf(rstds[g], inv, a.eps)));
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     const int p = k.row + u * k.rows;
@@ -217,21 +219,20 @@ __global__ __launch_bounds__(kMost<TI>) void last_stats(NormArgs a) {
         s[j] = fmaf(d, d, s[j]);
       }
     };
-    int i = 0;
-    {
-      const raw4 r = load(0);
-#pragma unroll
-      for (int j = 0; j < V; ++j) about[j] = element<TI>(r, j);
-    }
-    for (; i + 4 <= count; i += 4, at += 4 * step) {
+    for (int i = 0; i < count; i += 4, at += 4 * step) {
       raw4 r[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) r[u] = load(u);
+      for (int u = 0; u < 4; ++u)
+        if (i + u < count) r[u] = load(u);
+      if (i == 0) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) add(r[u]);
+        for (int j = 0; j < V; ++j) about[j] = element<TI>(r[0], j);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (i + u < count) add(r[u]);
     }
-    for (; i < count; ++i, at += step) add(load(0));
-    const float inv = 1.0f / (float)count;
+    const float inv = inverse((float)count);
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float d = m[j] * inv;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(kMost<TI>) void last_stats(NormArgs a) {
 #pragma unroll
   for (int j = 0; j < V; ++j) v[j] = m[j] * (float)count;
   slab_sums<V>(a, k.groups, v, rows, means);
-  const float pixels = (float)(last - first), inv = 1.0f / ((float)a.cpg * pixels);
+  const float pixels = (float)(last - first), inv = inverse((float)a.cpg * pixels);
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const float d = m[j] - means[group[j]] * inv;
@@ -307,15 +308,15 @@ __global__ __launch_bounds__(kMost<TI>) void last_apply(NormArgs a) {
     activate<V>(a.activation, z);
     store_out<TO, V>(a, y + to + u * step_y, z, WHOLE ? V : k.valid);
   };
-  int i = 0;
-  for (; i + 4 <= count; i += 4, at += 4 * step, to += 4 * step_y) {
+  for (int i = 0; i < count; i += 4, at += 4 * step, to += 4 * step_y) {
     raw4 r[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) r[u] = load(u);
+    for (int u = 0; u < 4; ++u)
+      if (i + u < count) r[u] = load(u);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) store(u, r[u]);
+    for (int u = 0; u < 4; ++u)
+      if (i + u < count) store(u, r[u]);
   }
-  for (; i < count; ++i, at += step, to += step_y) store(0, load(0));
 }
 
 // ---- backward ----
@@ -450,7 +451,7 @@ __global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   T* dx = static_cast<T*>(a.y) + n * a.xs_n + k.c;
   const int64_t room = a.x_end - n * a.xs_n - k.c, room_y = a.y_end - n * a.ys_n - k.c;
   float2* means = reinterpret_cast<float2*>(lds);
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float inv = inverse((float)a.cpg * (float)a.P);
   const int width = lanes_of(k.groups), lane = threadIdx.x & (width - 1);
   for (int g = threadIdx.x / width; g < k.groups; g += (int)blockDim.x / width) {
     const float2* part = reinterpret_cast<const float2*>(a.part) + ((int64_t)n * a.G + k.g0 + g) * a.chunks;
@@ -542,15 +543,16 @@ size_t plan_norm_last(NormArgs* a, int x_size, bool resident_allowed) {
   set_slab(a, wide, V);
   a->chunks = 1;
   a->per = a->P;
+  const int64_t cells = (int64_t)a->N * a->slabs;
   for (int threads = 64; resident_allowed && threads <= 1024; threads *= 2) {
     const int rows = threads >> a->lanes;
     if (rows == 0) continue;
     const int64_t each = ((int64_t)a->P + rows - 1) / rows;
-    if (each > (threads < 1024 ? 4 : 8)) continue;
+    if (each > (threads < 1024 ? 4 : 8)) continue;  // (a thread has up to four vectors before the workgroup grows)
     a->threads = threads;
     a->per_thread = each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
     // (few slabs over long maps leave most of the chip idle)
-    if ((int64_t)a->N * a->slabs >= 128 || each * threads <= 2048) return 0;
+    if (cells >= 128 || each * threads <= 2048) return 0;
   }
   set_parts(a, x_size);
   return (size_t)a->N * a->G * a->chunks * 16;

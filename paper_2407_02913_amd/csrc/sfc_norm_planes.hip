@@ -87,7 +87,7 @@ __global__ __launch_bounds__(1024) void planes_resident(NormArgs a) {
   for (int u = 0; u < NV; ++u)
 #pragma unroll
     for (int j = 0; j < V; ++j) sum += element<TI>(raw[u], j);
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float inv = inverse((float)a.cpg * (float)a.P);
   const float mean = block_sum(sum, scratch) * inv;
   float squares = 0.0f;
 #pragma unroll
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(1024) void planes_resident(NormArgs a) {
     }
   }
   const float var = block_sum(squares, scratch + 16) * inv;
-  const float2 stat = make_float2(mean, 1.0f / sqrtf(var + a.eps));
+  const float2 stat = make_float2(mean, inverse_sqrt(var + a.eps));
   if (t == 0) reinterpret_cast<float2*>(a.stats)[blockIdx.x] = stat;
   TO* y = static_cast<TO*>(a.y) + y0;
 #pragma unroll
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(1024) void planes_back_resident(NormArgs a) {
   }
   __syncthreads();
   const float2 sums = group_of_channels(a, channels, wb);
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float inv = inverse((float)a.cpg * (float)a.P);
   const float c1 = sums.x * inv, c2 = sums.y * inv;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -436,7 +436,7 @@ __global__ __launch_bounds__(256) void planes_back_apply(NormArgs a) {
     const float2 v = reinterpret_cast<const float2*>(a.part)[ng * a.chunks + i];
     s.x += v.x, s.y += v.y;
   }
-  const float inv = 1.0f / ((float)a.cpg * (float)a.P);
+  const float inv = inverse((float)a.cpg * (float)a.P);
   const float c1 = wave_sum(s.x) * inv, c2 = wave_sum(s.y) * inv;
   __syncthreads();
   for (int q = first + threadIdx.x; q < last; q += 512) {
@@ -482,7 +482,7 @@ void cut_into_vectors(NormArgs* a, int x_size, bool dense) {
 void choose_resident(NormArgs* a, int64_t items, int most) {
   a->threads = a->per_thread = 0;
   for (int threads = 64; threads <= 1024; threads *= 2) {
-    // (a thread with up to four vectors before the workgroup grows)
+    // (a thread has up to four vectors before the workgroup grows)
     if (items <= (int64_t)threads * (threads < 1024 ? 4 : most)) {
       a->threads = threads;
       int nv = 1;
