@@ -8,7 +8,7 @@
 // The logits are the largest tensor of a training step, and a row's gradient needs the whole row's sum: a row is
 // kept in registers as it was loaded (distill_rows: by a wave up to 256 vectors of 16 bytes, by a workgroup above),
 // so that loss and gradient read it once and write it once.  Rows past the registers are read twice, the second time
-// mostly out of the caches (distill_stream).  The gradient is stored as if there were no teacher, then the wave that
+// mostly out of the caches (distill_stream), and so are those of calls that gain nothing by keeping them (run_distill).  The gradient is stored as if there were no teacher, then the wave that
 // stored a place's vector stores that place once more.  With a tail the sum outside the top is added up as such (a
 // difference of sums would lose it where the top holds nearly all): a byte of LDS a vector tells its elements.
 #include "sfc_distill.hpp"
@@ -184,10 +184,10 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
   return make_float2(mass, log_sum);
 }
 
-// exp((s - max) / T) with c = log2 e / T and top = max c rounded: what that rounding is worth multiplies all of a row's
-// exponentials alike and leaves their ratios.
-__device__ __forceinline__ float scaled_exp(float s, float c, float top) {
-  return __builtin_amdgcn_exp2f(fmaf(s, c, -top));
+// exp((s - max) / T) with c = log2 e / T.  (The difference first: max c by itself may leave float32's range, where a row
+// or a thread has nothing but its type's lowest value so far.)
+__device__ __forceinline__ float scaled_exp(float s, float c, float max) {
+  return __builtin_amdgcn_exp2f((s - max) * c);
 }
 
 // The elements of this lane's vector that are the teacher's.
@@ -201,7 +201,7 @@ __device__ __forceinline__ void gradient(const DistillArgs& a, const Row& row, f
                                          float (&v)[kVec<T>]) {
   const float c = kLog2e / a.temperature, unit = scale / row.sum * (row.mass - row.ratio);
 #pragma unroll
-  for (int j = 0; j < kVec<T>; ++j) v[j] = scaled_exp(element<T>(raw, j), c, row.max * c) * unit;
+  for (int j = 0; j < kVec<T>; ++j) v[j] = scaled_exp(element<T>(raw, j), c, row.max) * unit;
 }
 
 // The gradient at the teacher's places, by the wave whose lanes stored their vectors: a wave's stores to one address
@@ -218,7 +218,7 @@ __device__ __forceinline__ void store_places(const DistillArgs& a, const RowSpac
   for (int k = threadIdx.x & 63; k < a.top; k += 64) {
     const int place = s.at[k];
     if (place < 0 || (LANES > 64 && place / V % LANES / 64 != (int)(threadIdx.x >> 6))) continue;
-    const float q = scaled_exp(s.logit[k], c, row.max * c) / row.sum;
+    const float q = scaled_exp(s.logit[k], c, row.max) / row.sum;
     grad[place] = (T)((q * row.mass - s.all[k]) * scale);
   }
 }
@@ -241,7 +241,7 @@ __device__ __forceinline__ void add_exp(const DistillArgs& a, const RowSpace& s,
   const float c = kLog2e / a.temperature;
   float e[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) e[j] = scaled_exp(element<T>(raw, j), c, max * c);
+  for (int j = 0; j < V; ++j) e[j] = scaled_exp(element<T>(raw, j), c, max);
   if (a.tail) {
     const unsigned mask = live ? top_elements(s, item) : 0u;
     if (mask) {
@@ -356,7 +356,7 @@ __device__ __forceinline__ float largest(raw4 (&raw)[NV]) {
 // scalar for the team and a lane's offset, so that the registers are the row's; the vector that the row's end cuts, if
 // any, is loaded and stored by itself.
 template <typename T, int NV, int LANES, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? 4 : NV == 8 ? 5 : 2) void distill_rows(DistillArgs a, int space) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256 ? 3 : 4) : NV == 8 ? 4 : 2) void distill_rows(DistillArgs a, int space) {
   constexpr int V = kVec<T>;
   constexpr int TEAMS = LANES == 64 ? 4 : 1;
   extern __shared__ float4 lds[];
@@ -462,28 +462,28 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? 4 : NV == 8 ?
 }
 
 // A row to a workgroup, read once for its sums and once more for the gradient.
-template <typename T>
-__global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
+template <typename T, int LANES>
+__global__ __launch_bounds__(LANES) void distill_stream(DistillArgs a) {
   constexpr int V = kVec<T>;
   extern __shared__ float4 lds[];
   const int64_t row = blockIdx.x;
   const RowSpace s = row_space(reinterpret_cast<char*>(lds), a.top);
-  Team<1024> team{s.scratch};
+  Team<LANES> team{s.scratch};
   const float scale = a.row_scale ? a.row_scale[row] : 1.0f;
   if (scale == 0.0f) {
-    masked_row<T, 1024>(a, row, team);
+    masked_row<T, LANES>(a, row, team);
     return;
   }
   const T* logits = static_cast<const T*>(a.logits) + row * a.logits_stride;
   const int64_t room = (a.rows - 1 - row) * a.logits_stride + a.classes;
-  const int items = (a.classes + V - 1) / V, lane = threadIdx.x, size = 1024;
+  const int items = (a.classes + V - 1) / V, lane = threadIdx.x, size = LANES;
   auto load = [&](int q) {
     if (q >= items) return raw4{kNone<T>, kNone<T>, kNone<T>, kNone<T>};
     return load_cut(logits + (int64_t)q * V, a.classes - q * V, room - (int64_t)q * V, kNone<T>);
   };
   Entry entry = load_entry(a, row, lane);
   if (entry.place >= 0) entry.logit = (float)logits[entry.place];
-  const float2 teacher = stage_teacher<T, 1024>(a, row, s, team, logits, entry);
+  const float2 teacher = stage_teacher<T, LANES>(a, row, s, team, logits, entry);
   Row r;
   if (a.loss) {
     // each thread its own running maximum, its sums scaled down when that grows
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
     rest = team.sum(rest * f);
     top = a.tail ? team.sum(top * f) : 0.0f;
     if (m == -INFINITY) rest = NAN;
-    r = finish_loss<1024>(a, row, s, team, teacher, m, rest, top);
+    r = finish_loss<LANES>(a, row, s, team, teacher, m, rest, top);
   } else {
     r = row_of_stats(a, row);
   }
@@ -533,7 +533,7 @@ __global__ __launch_bounds__(1024) void distill_stream(DistillArgs a) {
         if (q < items) store_vec<T, V>(grad + (int64_t)q * V, v, min(V, a.classes - q * V));
       }
     }
-    store_places<T, 1024>(a, s, team, r, scale * a.temperature, grad);
+    store_places<T, LANES>(a, s, team, r, scale * a.temperature, grad);
   }
 }
 
@@ -544,8 +544,20 @@ hipError_t run_rows(const DistillArgs& a, int items, int per_unit, hipStream_t s
   const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS, most = 256 * (int64_t)per_unit;
   const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(LANES == 64 ? 256 : LANES);
   if (a.loss && a.grad) distill_rows<T, NV, LANES, true, true><<<grid, block, TEAMS * space, s>>>(a, space);
-  else if (a.loss) distill_rows<T, NV, LANES, true, false><<<grid, block, TEAMS * space, s>>>(a, space);
-  else distill_rows<T, NV, LANES, false, true><<<grid, block, TEAMS * space, s>>>(a, space);
+  else if (a.grad) distill_rows<T, NV, LANES, false, true><<<grid, block, TEAMS * space, s>>>(a, space);
+  else if constexpr (LANES == 64) distill_rows<T, NV, LANES, true, false><<<grid, block, TEAMS * space, s>>>(a, space);
+  return hipGetLastError();
+}
+
+template <typename T, int LANES>
+hipError_t run_stream(const DistillArgs& a, int items, hipStream_t s) {
+  const int space = row_space_bytes(a.top, items, a.tail);
+  if (space > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(distill_stream<T, LANES>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, space);
+    if (e != hipSuccess) return e;
+  }
+  distill_stream<T, LANES><<<dim3((unsigned)a.rows), LANES, space, s>>>(a);
   return hipGetLastError();
 }
 
@@ -556,19 +568,18 @@ hipError_t run_distill(const DistillArgs& a, hipStream_t s) {
   if (items <= 64) return run_rows<T, 1, 64>(a, items, 8, s);
   if (items <= 128) return run_rows<T, 2, 64>(a, items, 8, s);
   if (items <= 256) return run_rows<T, 4, 64>(a, items, 6, s);
-  if (items <= 1024) return run_rows<T, 4, 256>(a, items, 6, s);
+  // Rows that are read again: where there are too few for the others to work in a pipeline, the more waves the better
+  // (64 rows of 32000 classes in 16 bits, loss and gradient: 12.7 us, kept in registers 14.1; 300 of 131072: 52 and 66).
+  if (a.rows <= 512 || items > 16384) return run_stream<T, 512>(a, items, s);
+  // Small workgroups, a row each, hide each other's waiting where little would be saved by keeping the row.  The loss
+  // alone reads it once either way (4096 rows of 65536: 98 us, kept in registers 124).  The gradient alone needs no sums
+  // (777 rows of 32003: 25 and 29, 4096 rows of 16384: 60 and 65; but 4096 rows of 32000: 123 and 107).  Both: short
+  // rows (4096 rows of 6000: 41 and 46; of 16384: 75 and 71, of 131072: 660 and 532).
+  if (!a.grad || (!a.loss ? items <= 2048 || a.rows <= 1024 : items <= 1024)) return run_stream<T, 256>(a, items, s);
   if (items <= 2048) return run_rows<T, 8, 256>(a, items, 4, s);
-  if (items <= 4096) return run_rows<T, 16, 256>(a, items, 4, s);
+  if (items <= 4096) return run_rows<T, 16, 256>(a, items, 3, s);
   if (items <= 8192) return run_rows<T, 16, 512>(a, items, 2, s);
-  if (items <= 16384) return run_rows<T, 32, 512>(a, items, 1, s);
-  const int space = row_space_bytes(a.top, items, a.tail);
-  if (space > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(distill_stream<T>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, space);
-    if (e != hipSuccess) return e;
-  }
-  distill_stream<T><<<dim3((unsigned)a.rows), dim3(1024), space, s>>>(a);
-  return hipGetLastError();
+  return run_rows<T, 32, 512>(a, items, 1, s);
 }
 
 }  // namespace

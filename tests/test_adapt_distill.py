@@ -203,6 +203,30 @@ def test_the_largest_logit_is_found_everywhere(classes, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,classes", [(3, 40), (3, 1001), (3, 70001), (600, 9001), (600, 2500)])
+def test_rows_of_the_lowest_value(rows, classes, dtype):
+    """Rows whose classes are masked with the type's lowest value, all of them or all but one: a uniform student, and a
+    certain one."""
+    from paper_2407_02913_amd import adapt
+
+    for temperature in (1.0, 2.0):
+        _, values, index, _ = make((rows, classes, 5), dtype, False, 8)
+        logits = torch.full((rows, classes), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+        logits[1, index[1, 2]] = 1.0
+        loss, grad = adapt.distill_loss_and_grad(logits, values, index, temperature=temperature)
+        again, stats = adapt.distill_loss(logits, values, index, temperature=temperature)
+        apart = adapt.distill_grad(logits, values, index, stats, temperature=temperature)
+        want = definition(logits, values, index, temperature, False)
+        ones = torch.ones(rows, device="cuda")
+        kept = torch.arange(rows, device="cuda") != 1  # (row 1's loss is past float32 where the type's range is)
+        check((loss[kept], grad[kept]), [w[kept] for w in want], dtype, ones[kept], temperature)
+        check((again[kept], apart[kept]), [w[kept] for w in want], dtype, ones[kept], temperature)
+        tol = 1e-5 * (want[3] + want[4]) * temperature + STEP[dtype] * want[1].abs() + 2.0 ** -25
+        assert ((grad.double() - want[1]).abs() <= tol)[1].all() and ((apart.double() - want[1]).abs() <= tol)[1].all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("classes", [600, 20000])
 def test_the_rest_of_a_certain_student(classes):
     """A student who has all but 1e-9 of its mass on the top: the rest is summed as such, not as a difference."""
