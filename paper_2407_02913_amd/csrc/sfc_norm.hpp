@@ -45,10 +45,17 @@ struct NormArgs {
   bool stream;             // the result is stored past the caches
 };
 
-// 1 / v and 1 / sqrt(v) of the hardware, within a unit of the last place: a wave of a small call waits for every
-// instruction, and the exact ones take some tens.
-__device__ __forceinline__ float inverse(float v) { return __builtin_amdgcn_rcpf(v); }
-__device__ __forceinline__ float inverse_sqrt(float v) { return __builtin_amdgcn_rsqf(v); }
+// 1 / v and 1 / sqrt(v): the hardware's, within a unit of the last place, and a step of Newton's method.  (A wave of a
+// small call waits for every instruction, and the exact ones take some tens.)
+__device__ __forceinline__ float inverse(float v) {
+  const float r = __builtin_amdgcn_rcpf(v);
+  return fmaf(fmaf(-v, r, 1.0f), r, r);
+}
+__device__ __forceinline__ float inverse_sqrt(float v) {
+  const float r = __builtin_amdgcn_rsqf(v);
+  const float s = fmaf(0.5f * r, fmaf(-v * r, r, 1.0f), r);
+  return s == s ? s : r;  // (0, infinity and NaN as the hardware has them)
+}
 
 // y = act(z)
 __device__ __forceinline__ float fast_sigmoid(float z) {

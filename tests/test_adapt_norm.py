@@ -230,6 +230,28 @@ def test_a_broken_value_stays_in_its_group(layout, value, shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("shape", [(3, 46, 7, 9, 2), (1, 24, 131, 127, 1), (2, 64, 56, 56, 32)])
+def test_in_place_through_the_c_entry(layout, shape):
+    from paper_2407_02913_amd import adapt, binding
+
+    n, c, h, w, groups = shape
+    x, weight, bias, _ = make(shape, torch.bfloat16, layout, seed=7)
+    want, _ = adapt.group_norm_forward(x, groups, weight, bias, activation="silu")
+    code = 1 if layout == "nhwc" else 0
+    d = _desc(N=n, C=c, H=h, W=w, groups=groups, x_type=2, y_type=2, x_layout=code, y_layout=code, activation=2)
+    need = C.c_size_t()
+    lib = binding.load()
+    assert lib.sfc_group_norm_sizes(C.addressof(d), C.byref(need), None) == 0
+    stats = torch.empty(n, groups, 2, device="cuda")
+    space = binding.device_buffer(need.value)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.sfc_group_norm(C.addressof(d), x.data_ptr(), weight.data_ptr(), bias.data_ptr(), x.data_ptr(), stats.data_ptr(),
+                              space.data_ptr(), need.value, stream) == 0
+    assert torch.equal(x, want)
+
+
+@pytest.mark.gpu
 def test_one_value_to_a_group_has_no_gradient():
     from paper_2407_02913_amd import adapt
 
