@@ -297,12 +297,19 @@ __device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, co
   return r;
 }
 
-// A row whose scale is zero: nothing of it is read.
+// A row's scale, zero where it is masked, here or (a mass of -1) in the call that left its statistics.
+template <bool LOSS>
+__device__ __forceinline__ float scale_of(const DistillArgs& a, int64_t row) {
+  if (!LOSS && a.stats[4 * row + 3] < 0.0f) return 0.0f;
+  return a.row_scale ? a.row_scale[row] : 1.0f;
+}
+
+// A masked row: nothing of it is read.
 template <typename T, int LANES>
 __device__ __forceinline__ void masked_row(const DistillArgs& a, int64_t row, Team<LANES>& team) {
   if (a.loss && team.lane() == 0) {
     a.loss[row] = 0.0f;
-    if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(0.0f, 1.0f, 0.0f, 0.0f);
+    if (a.stats) reinterpret_cast<float4*>(a.stats)[row] = make_float4(0.0f, 1.0f, 0.0f, -1.0f);
   }
   if (a.grad) {
     T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
   // The first row from `row` on that is not masked; masked ones on the way are done with.
   float scale = 1.0f;
   auto unmasked = [&](int64_t row) {
-    while (row < a.rows && a.row_scale && (scale = uniform(a.row_scale[row])) == 0.0f) {
+    while (row < a.rows && (a.row_scale || !LOSS) && (scale = uniform(scale_of<LOSS>(a, row))) == 0.0f) {
       masked_row<T, LANES>(a, row, team);
       row += rows_step;
     }
@@ -469,7 +476,7 @@ __global__ __launch_bounds__(LANES) void distill_stream(DistillArgs a) {
   const int64_t row = blockIdx.x;
   const RowSpace s = row_space(reinterpret_cast<char*>(lds), a.top);
   Team<LANES> team{s.scratch};
-  const float scale = a.row_scale ? a.row_scale[row] : 1.0f;
+  const float scale = a.loss ? scale_of<true>(a, row) : scale_of<false>(a, row);
   if (scale == 0.0f) {
     masked_row<T, LANES>(a, row, team);
     return;

@@ -203,6 +203,22 @@ def test_the_largest_logit_is_found_everywhere(classes, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(5, 40), (5, 3000), (5, 200000), (600, 33000)])
+def test_a_row_masked_in_the_loss_stays_masked(rows, classes):
+    """Whatever it holds, and whatever scale the gradient's call gives it."""
+    from paper_2407_02913_amd import adapt
+
+    logits, values, index, _ = make((rows, classes, 5), torch.float32, False, 9)
+    mask = torch.ones(rows, device="cuda")
+    mask[1] = mask[3] = 0.0
+    logits[1], logits[3] = 500.0, math.nan
+    _, stats = adapt.distill_loss(logits, values, index, row_scale=mask)
+    for scale in (None, torch.full((rows,), 2.0, device="cuda")):
+        grad = adapt.distill_grad(logits, values, index, stats, row_scale=scale)
+        assert (grad[1] == 0).all() and (grad[3] == 0).all() and (grad[0] != 0).any() and torch.isfinite(grad).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows,classes", [(3, 40), (3, 1001), (3, 70001), (600, 9001), (600, 2500)])
 def test_rows_of_the_lowest_value(rows, classes, dtype):
