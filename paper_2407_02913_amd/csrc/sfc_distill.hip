@@ -101,21 +101,30 @@ struct Row {
   float mass;             // sum of the teacher's probabilities, the rest included
 };
 
-// One of a row's entries: place (-1: none), value, and the student's logit there.
+// One of a row's entries: as it is loaded, and its place (-1: none) and the student's logit there.
 struct Entry {
+  int2 index;
+  float value;
   int place;
-  float value, logit;
+  float logit;
 };
 
+// (Nothing here waits for what is loaded: find_logit does.)
 __device__ __forceinline__ Entry load_entry(const DistillArgs& a, int64_t row, int k) {
-  Entry e = {-1, 0.0f, 0.0f};
+  Entry e = {make_int2(-1, -1), 0.0f, -1, 0.0f};
   if (k < a.top) {
-    const int64_t at = a.wide ? static_cast<const int64_t*>(a.index)[row * a.index_stride + k]
-                              : static_cast<const int32_t*>(a.index)[row * a.index_stride + k];
-    e.place = at >= 0 && at < a.classes ? (int)at : -1;
+    const int* at = static_cast<const int*>(a.index) + ((row * a.index_stride + k) << (int)a.wide);
+    e.index = make_int2(at[0], at[a.wide ? 1 : 0]);
     e.value = a.values[row * a.values_stride + k];
   }
   return e;
+}
+
+template <typename T>
+__device__ __forceinline__ void find_logit(const DistillArgs& a, const T* logits, Entry& e) {
+  const bool in = e.index.x >= 0 && e.index.x < a.classes && (!a.wide || e.index.y == 0);
+  e.place = in ? e.index.x : -1;
+  if (in) e.logit = (float)logits[e.place];
 }
 
 // The teacher's entries into LDS (a place outside the classes is none) and, with a tail, the map of vectors that hold
@@ -132,20 +141,22 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
     team.sync();
   }
   float top = -INFINITY;
+  auto put = [&](int k, const Entry& e) {
+    s.at[k] = e.place;
+    s.p[k] = s.value[k] = e.value;
+    if (e.place >= 0) {
+      s.logit[k] = e.logit;
+      top = fmaxf(top, e.value);
+      if (a.tail) atomicOr(&s.map[e.place / (4 * V)], 1u << (e.place / V % 4 * 8 + e.place % V));
+    }
+  };
+  // (the lane's first one by itself: a wait for loads in the loop would be one for the row's logits, too)
+  if (lane < a.top) put(lane, own);
 #pragma unroll 1
-  for (int k = lane; k < a.top; k += size) {
-    if (k != lane) {
-      own = load_entry(a, row, k);
-      if (own.place >= 0) own.logit = (float)logits[own.place];
-    }
-    const int place = own.place;
-    s.at[k] = place;
-    s.p[k] = s.value[k] = own.value;
-    if (place >= 0) {
-      s.logit[k] = own.logit;
-      top = fmaxf(top, own.value);
-      if (a.tail) atomicOr(&s.map[place / (4 * V)], 1u << (place / V % 4 * 8 + place % V));
-    }
+  for (int k = lane + size; k < a.top; k += size) {
+    Entry e = load_entry(a, row, k);
+    find_logit(a, logits, e);
+    put(k, e);
   }
   float about = 0.0f, log_sum = 0.0f, c = 1.0f, scale = 1.0f;
   if (!a.tail) {
@@ -190,11 +201,6 @@ __device__ __forceinline__ float scaled_exp(float s, float c, float max) {
   return __builtin_amdgcn_exp2f((s - max) * c);
 }
 
-// The elements of this lane's vector that are the teacher's.
-__device__ __forceinline__ unsigned top_elements(const RowSpace& s, int item) {
-  return s.map[item >> 2] >> (item & 3) * 8 & 255u;
-}
-
 // The gradient of a vector outside the teacher's places.
 template <typename T>
 __device__ __forceinline__ void gradient(const DistillArgs& a, const Row& row, float scale, const raw4& raw,
@@ -233,9 +239,9 @@ __device__ __forceinline__ void store_nothing(const DistillArgs& a, int item, T*
 }
 
 // Sums of exp((s - max) / T) of a vector: of the elements outside the teacher's places and, with a tail, of those
-// on them (else of all).
+// on them (else of all).  The byte at `shift` of `map` tells which those are.
 template <typename T>
-__device__ __forceinline__ void add_exp(const DistillArgs& a, const RowSpace& s, const raw4& raw, int item, bool live,
+__device__ __forceinline__ void add_exp(const DistillArgs& a, const unsigned* map, int shift, const raw4& raw, bool live,
                                         float max, float* rest, float* top) {
   constexpr int V = kVec<T>;
   const float c = kLog2e / a.temperature;
@@ -243,7 +249,7 @@ __device__ __forceinline__ void add_exp(const DistillArgs& a, const RowSpace& s,
 #pragma unroll
   for (int j = 0; j < V; ++j) e[j] = scaled_exp(element<T>(raw, j), c, max);
   if (a.tail) {
-    const unsigned mask = live ? top_elements(s, item) : 0u;
+    const unsigned mask = live ? *map >> shift & 255u : 0u;
     if (mask) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
@@ -255,6 +261,72 @@ __device__ __forceinline__ void add_exp(const DistillArgs& a, const RowSpace& s,
   }
 #pragma unroll
   for (int j = 0; j < V; ++j) *rest += e[j];
+}
+
+// The largest element of NV vectors.  16-bit types: two at a time as integers, which order like the floats where the
+// largest is not negative (and a negative result tells that it was).
+template <typename T, int NV>
+__device__ __forceinline__ float largest(raw4* raw) {
+  constexpr int V = kVec<T>;
+  if constexpr (sizeof(T) == 2) {
+    typedef short s2 __attribute__((ext_vector_type(2)));
+    s2 m = {-32768, -32768};
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        const unsigned two = raw[u][d];  // (a copy: a bit cast of the vector's element itself takes the first one)
+        m = __builtin_elementwise_max(m, __builtin_bit_cast(s2, two));
+      }
+    const short top = m[0] > m[1] ? m[0] : m[1];
+    if (top >= 0) return (float)__builtin_bit_cast(T, top);
+  }
+  float max = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(raw[u], j));
+    asm volatile("" : "+v"(raw[u]));  // (the loaded bits are kept, not the floats made of them)
+  }
+  return max;
+}
+
+// A thread's largest logit so far, and the sums of exp((s - max) / T) about it.
+struct Running {
+  float max = -INFINITY, rest = 0.0f, top = 0.0f;
+};
+
+// NV vectors more, of items `item` + from, + from + step, ...: the sums are scaled down where the maximum grows.  (So the first
+// vectors of a row are worked on while its last ones are on their way.)
+template <typename T, int NV>
+__device__ __forceinline__ void add_vectors(const DistillArgs& a, const RowSpace& s, raw4* raw, int item, int from,
+                                            int step, int items, Running& run) {
+  const float m = fmaxf(run.max, largest<T, NV>(raw));
+  if (m > run.max) {
+    const float f = __builtin_amdgcn_exp2f((run.max - m) * (kLog2e / a.temperature));
+    run.rest *= f, run.top *= f;
+    run.max = m;
+  }
+  const unsigned* map = s.map + item / 4;  // (steps are multiples of four)
+  // (nothing but -inf so far counts for nothing; a NaN makes the sums one)
+  const float about = run.max == -INFINITY ? 0.0f : run.max;
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    add_exp<T>(a, map + (from + u * step) / 4, item % 4 * 8, raw[u], item + from + u * step < items, about, &run.rest, &run.top);
+    asm volatile("" : "+v"(raw[u]));  // (the loaded bits are kept, not the floats made of them)
+  }
+}
+
+// The team's sums, about the row's largest logit.
+template <int LANES>
+__device__ __forceinline__ Running join(const DistillArgs& a, Team<LANES>& team, Running run) {
+  const float m = team.max(run.max);
+  const float f = run.max == m ? 1.0f : __builtin_amdgcn_exp2f((run.max - m) * (kLog2e / a.temperature));
+  run.max = m;
+  run.rest = team.sum(run.rest * f);
+  run.top = a.tail ? team.sum(run.top * f) : 0.0f;
+  if (m == -INFINITY) run.rest = NAN;
+  return run;
 }
 
 // Loss and statistics once the student's sums stand.
@@ -297,11 +369,17 @@ __device__ __forceinline__ Row finish_loss(const DistillArgs& a, int64_t row, co
   return r;
 }
 
+// A value of a row, by a scalar load: it does not stand in line behind the row's logits.
+__device__ __forceinline__ float of_row(const float* from, int64_t at) {
+  typedef const __attribute__((address_space(4))) float* Scalar;
+  return *reinterpret_cast<Scalar>(reinterpret_cast<uintptr_t>(from + at));
+}
+
 // A row's scale, zero where it is masked, here or (a mass of -1) in the call that left its statistics.
 template <bool LOSS>
 __device__ __forceinline__ float scale_of(const DistillArgs& a, int64_t row) {
-  if (!LOSS && a.stats[4 * row + 3] < 0.0f) return 0.0f;
-  return a.row_scale ? a.row_scale[row] : 1.0f;
+  if (!LOSS && of_row(a.stats, 4 * row + 3) < 0.0f) return 0.0f;
+  return a.row_scale ? of_row(a.row_scale, row) : 1.0f;
 }
 
 // A masked row: nothing of it is read.
@@ -319,9 +397,9 @@ __device__ __forceinline__ void masked_row(const DistillArgs& a, int64_t row, Te
 }
 
 __device__ __forceinline__ Row row_of_stats(const DistillArgs& a, int64_t row) {
-  const float4 v = reinterpret_cast<const float4*>(a.stats)[row];
   Row r;
-  r.max = v.x, r.sum = v.y, r.ratio = v.z, r.mass = v.w;
+  r.max = of_row(a.stats, 4 * row), r.sum = of_row(a.stats, 4 * row + 1);
+  r.ratio = of_row(a.stats, 4 * row + 2), r.mass = of_row(a.stats, 4 * row + 3);
   return r;
 }
 
@@ -330,38 +408,13 @@ __device__ __forceinline__ float uniform(float v) {
   return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
 }
 
-// The largest element of NV vectors.  16-bit types: two at a time as integers, which order like the floats where the
-// largest is not negative (and a negative result tells that it was).
-template <typename T, int NV>
-__device__ __forceinline__ float largest(raw4 (&raw)[NV]) {
-  constexpr int V = kVec<T>;
-  if constexpr (sizeof(T) == 2) {
-    typedef short s2 __attribute__((ext_vector_type(2)));
-    s2 m = {-32768, -32768};
-#pragma unroll
-    for (int u = 0; u < NV; ++u)
-#pragma unroll
-      for (int d = 0; d < 4; ++d) {
-        const unsigned two = raw[u][d];  // (a copy: a bit cast of the vector's element itself takes the first one)
-        m = __builtin_elementwise_max(m, __builtin_bit_cast(s2, two));
-      }
-    const short top = m[0] > m[1] ? m[0] : m[1];
-    if (top >= 0) return (float)__builtin_bit_cast(T, top);
-  }
-  float max = -INFINITY;
-#pragma unroll
-  for (int u = 0; u < NV; ++u) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(raw[u], j));
-    asm volatile("" : "+v"(raw[u]));  // (the loaded bits are kept, not the floats made of them)
-  }
-  return max;
-}
-
 // A row to a team, NV vectors to a lane.  A team takes every gridDim.x-th row, and loads a vector of its next one as soon
-// as the gradient of that vector has left: reading runs beside the exponentials and the writing.  Addresses are a
-// scalar for the team and a lane's offset, so that the registers are the row's; the vector that the row's end cuts, if
-// any, is loaded and stored by itself.
+// as the gradient of that vector has left: reading runs beside the exponentials and the writing.  A wave's loads and
+// stores are counted in one line, and it can wait for the ones at its front only where their number is known when this
+// is compiled: a workgroup's loads have no branches (more than half of its NV vectors are the row's for every lane, or
+// a smaller NV had been taken), and what else a row needs is loaded ahead of its logits or by scalar loads.
+// Addresses are a scalar for the team and a lane's offset, so that the registers are the row's; the vector that the
+// row's end cuts, if any, is loaded and stored by itself.
 template <typename T, int NV, int LANES, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256 ? 3 : 4) : NV == 8 ? 4 : 2) void distill_rows(DistillArgs a, int space) {
   constexpr int V = kVec<T>;
@@ -371,18 +424,21 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
   const int64_t first = (int64_t)blockIdx.x * TEAMS + mine, rows_step = (int64_t)gridDim.x * TEAMS;
   const RowSpace s = row_space(reinterpret_cast<char*>(lds) + mine * space, a.top);
   Team<LANES> team{s.scratch};
-  const int lane = team.lane(), rest_elements = a.classes % V, whole = a.classes / V;
-  // Vectors u < full are whole for every lane, of vector `full` the first `ragged` lanes' are; the element count's rest
-  // lies behind them, with one lane.
-  const int full = whole / LANES, ragged = whole - full * LANES;
-  const bool cuts = rest_elements != 0 && lane == ragged;
+  const int lane = team.lane(), rest_elements = a.classes % V, whole = a.classes / V, items = whole + (rest_elements != 0);
+  // Vectors u < full are whole for every lane, of vector `full` some lanes' are; the element count's rest lies behind
+  // them, with one lane.
+  const int full = whole / LANES;
+  const bool cuts = rest_elements != 0 && lane == whole - full * LANES;
   const unsigned offset = (unsigned)lane * V;
   constexpr raw4 none = {kNone<T>, kNone<T>, kNone<T>, kNone<T>};
+  auto mine_too = [&](int u) { return (LANES > 64 && u < NV / 2) || u * LANES + lane < whole; };
   auto load = [&](const T* at, int u) {
-    raw4 r = none;
-    if (u < full) r = load16(at + u * LANES * V + offset);
-    else if (u == full && lane < ragged) r = load16(at + u * LANES * V + offset);
-    return r;
+    if constexpr (LANES == 64) {
+      return mine_too(u) ? load16(at + u * LANES * V + offset) : none;
+    } else {
+      // (lanes past the row's end take its first vector, and drop it where they add)
+      return load16(at + (mine_too(u) ? u * LANES * V + offset : 0u));
+    }
   };
   auto load_the_cut = [&](int64_t row, const T* at) {
     return cuts ? load_cut(at + whole * V, rest_elements, (a.rows - 1 - row) * a.logits_stride + rest_elements, kNone<T>)
@@ -405,10 +461,13 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
   Entry entry = load_entry(a, row, lane);
   {
     const T* at = row_at(row);
-#pragma unroll
-    for (int u = 0; u < NV; ++u) raw[u] = load(at, u);
+    find_logit(a, at, entry);
     cut = load_the_cut(row, at);
-    if (entry.place >= 0) entry.logit = (float)at[entry.place];
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      raw[u] = load(at, u);
+      __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop below)
+    }
   }
   for (;;) {
     const float unit = scale * a.temperature;
@@ -421,47 +480,50 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
     entry = load_entry(a, then, lane);
     Row r;
     if constexpr (LOSS) {
-      float max = largest<T, NV>(raw);
+      constexpr int EACH = NV < 2 ? NV : 2;
+      Running run;
 #pragma unroll
-      for (int j = 0; j < V; ++j) max = fmaxf(max, element<T>(cut, j));
-      max = team.max(max);
-      float rest = 0.0f, top = 0.0f;
+      for (int u = 0; u < NV; u += EACH) {
+        if (u > full) continue;
+        if constexpr (LANES > 64) {
 #pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        if (u <= full) add_exp<T>(a, s, raw[u], lane + u * LANES, u < full || lane < ragged, max, &rest, &top);
-        asm volatile("" : "+v"(raw[u]));
+          for (int i = u; i < u + EACH; ++i)
+            if (!mine_too(i)) raw[i] = none;
+        }
+        add_vectors<T, EACH>(a, s, raw + u, lane, u * LANES, LANES, whole, run);
       }
-      if (rest_elements) add_exp<T>(a, s, cut, whole, cuts, max, &rest, &top);
-      rest = team.sum(rest);
-      if (a.tail) top = team.sum(top);
-      r = finish_loss<LANES>(a, row, s, team, teacher, max, rest, a.tail ? top : 0.0f);
+      if (rest_elements) add_vectors<T, 1>(a, s, &cut, whole, 0, 0, cuts ? items : 0, run);
+      find_logit(a, next_at, entry);
+      run = join<LANES>(a, team, run);
+      r = finish_loss<LANES>(a, row, s, team, teacher, run.max, run.rest, run.top);
     } else {
+      find_logit(a, next_at, entry);
       r = row_of_stats(a, row);
     }
-    if (entry.place >= 0) entry.logit = (float)next_at[entry.place];
     if constexpr (GRAD) {
       T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
       float v[V];
+      gradient<T>(a, r, unit, cut, v);
+      if (cuts) store_vec<T, V>(grad + whole * V, v, rest_elements);
+      cut = load_the_cut(then, next_at);
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        if (u <= full) {
+        if ((LANES > 64 && u < NV / 2) || u <= full) {
           gradient<T>(a, r, unit, raw[u], v);
-          if (u < full || lane < ragged) {
+          if (mine_too(u)) {
             T* to = grad + u * LANES * V + offset;
             if (a.stream) store_vec<T, V, true>(to, v, V);
             else store_vec<T, V>(to, v, V);
           }
-          raw[u] = load(next_at, u);
         }
+        raw[u] = load(next_at, u);
       }
-      gradient<T>(a, r, unit, cut, v);
-      if (cuts) store_vec<T, V>(grad + whole * V, v, rest_elements);
       store_places<T, LANES>(a, s, team, r, unit, grad);
     } else {
+      cut = load_the_cut(then, next_at);
 #pragma unroll
       for (int u = 0; u < NV; ++u) raw[u] = load(next_at, u);
     }
-    cut = load_the_cut(then, next_at);
     if (next >= a.rows) return;
     row = next;
     team.sync();  // (the next row's teacher takes this one's place)
@@ -489,40 +551,19 @@ __global__ __launch_bounds__(LANES) void distill_stream(DistillArgs a) {
     return load_cut(logits + (int64_t)q * V, a.classes - q * V, room - (int64_t)q * V, kNone<T>);
   };
   Entry entry = load_entry(a, row, lane);
-  if (entry.place >= 0) entry.logit = (float)logits[entry.place];
+  find_logit(a, logits, entry);
   const float2 teacher = stage_teacher<T, LANES>(a, row, s, team, logits, entry);
   Row r;
   if (a.loss) {
-    // each thread its own running maximum, its sums scaled down when that grows
-    const float c = kLog2e / a.temperature;
-    float max = -INFINITY, rest = 0.0f, top = 0.0f;
+    Running run;
     for (int q0 = lane; q0 < items; q0 += 4 * size) {
       raw4 raw[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) raw[u] = load(q0 + u * size);
-      float m = max;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) m = fmaxf(m, element<T>(raw[u], j));
-      }
-      if (m > max) {
-        const float f = __builtin_amdgcn_exp2f((max - m) * c);
-        rest *= f, top *= f;
-        max = m;
-      }
-      // (nothing but -inf so far counts for nothing; a NaN makes the sums one)
-      const float about = max == -INFINITY ? 0.0f : max;
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        add_exp<T>(a, s, raw[u], q0 + u * size, q0 + u * size < items, about, &rest, &top);
+      add_vectors<T, 4>(a, s, raw, q0, 0, size, items, run);
     }
-    const float m = team.max(max);
-    const float f = max == m ? 1.0f : __builtin_amdgcn_exp2f((max - m) * c);
-    rest = team.sum(rest * f);
-    top = a.tail ? team.sum(top * f) : 0.0f;
-    if (m == -INFINITY) rest = NAN;
-    r = finish_loss<LANES>(a, row, s, team, teacher, m, rest, top);
+    run = join<LANES>(a, team, run);
+    r = finish_loss<LANES>(a, row, s, team, teacher, run.max, run.rest, run.top);
   } else {
     r = row_of_stats(a, row);
   }
@@ -585,7 +626,7 @@ hipError_t run_distill(const DistillArgs& a, hipStream_t s) {
   if (!a.grad || (!a.loss ? items <= 2048 || a.rows <= 1024 : items <= 1024)) return run_stream<T, 256>(a, items, s);
   if (items <= 2048) return run_rows<T, 8, 256>(a, items, 4, s);
   if (items <= 4096) return run_rows<T, 16, 256>(a, items, 3, s);
-  if (items <= 8192) return run_rows<T, 16, 512>(a, items, 2, s);
+  if (items <= 8192) return run_rows<T, 32, 256>(a, items, 2, s);
   return run_rows<T, 32, 512>(a, items, 1, s);
 }
 
