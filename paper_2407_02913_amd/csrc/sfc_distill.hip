@@ -422,7 +422,9 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
   extern __shared__ float4 lds[];
   const int mine = LANES == 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) : 0;
   const int64_t first = (int64_t)blockIdx.x * TEAMS + mine, rows_step = (int64_t)gridDim.x * TEAMS;
-  const RowSpace s = row_space(reinterpret_cast<char*>(lds) + mine * space, a.top);
+  constexpr int LAG = NV == 32 ? 8 : NV;  // vectors between a load and its sums, else all sums behind the loads
+  RowSpace s = row_space(reinterpret_cast<char*>(lds) + mine * 2 * space, a.top);
+  RowSpace other = row_space(reinterpret_cast<char*>(lds) + (mine * 2 + 1) * space, a.top);
   Team<LANES> team{s.scratch};
   const int lane = team.lane(), rest_elements = a.classes % V, whole = a.classes / V, items = whole + (rest_elements != 0);
   // Vectors u < full are whole for every lane, of vector `full` some lanes' are; the element count's rest lies behind
@@ -455,57 +457,68 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
     return row;
   };
   raw4 raw[NV], cut;
+  constexpr int EACH = NV < 2 ? NV : 2;
+  // Sums of the vectors from `u` on that are added at a time.
+  auto add = [&](const RowSpace& s, int u, Running& run) {
+    if (u > full) return;
+    if constexpr (LANES > 64) {
+#pragma unroll
+      for (int i = u; i < u + EACH; ++i)
+        if (!mine_too(i)) raw[i] = none;
+    }
+    add_vectors<T, EACH>(a, s, raw + u, lane, u * LANES, LANES, whole, run);
+  };
+  auto finish = [&](int64_t row, const RowSpace& s, float2 teacher, Running run) {
+    if (rest_elements) add_vectors<T, 1>(a, s, &cut, whole, 0, 0, cuts ? items : 0, run);
+    run = join<LANES>(a, team, run);
+    return finish_loss<LANES>(a, row, s, team, teacher, run.max, run.rest, run.top);
+  };
   int64_t row = unmasked(first);
   if (row >= a.rows) return;
-  // (a row's entries are asked for ahead of its logits, which would keep them waiting)
+  const float first_scale = scale;
   Entry entry = load_entry(a, row, lane);
-  {
-    const T* at = row_at(row);
-    find_logit(a, at, entry);
-    cut = load_the_cut(row, at);
+  find_logit(a, row_at(row), entry);
+  cut = load_the_cut(row, row_at(row));
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      raw[u] = load(at, u);
-      __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop below)
-    }
+  for (int u = 0; u < NV; ++u) {
+    raw[u] = load(row_at(row), u);
+    __builtin_amdgcn_sched_barrier(0);  // (in the order of the loop below)
   }
+  int64_t next = unmasked(row + rows_step);
+  float2 teacher = stage_teacher<T, LANES>(a, row, s, team, row_at(row), entry);
+  entry = load_entry(a, next < a.rows ? next : row, lane);
+  Row r;
+  if constexpr (LOSS) {
+    Running run;
+#pragma unroll
+    for (int u = 0; u < NV; u += EACH) add(s, u, run);
+    find_logit(a, row_at(next < a.rows ? next : row), entry);
+    r = finish(row, s, teacher, run);
+  } else {
+    find_logit(a, row_at(next < a.rows ? next : row), entry);
+    r = row_of_stats(a, row);
+  }
+  float unit = first_scale * a.temperature;
   for (;;) {
-    const float unit = scale * a.temperature;
-    const int64_t next = unmasked(row + rows_step);
     // (behind the last row: that row once more, for nothing, so that the loads have no condition)
     const int64_t then = next < a.rows ? next : row;
-    const T* next_at = row_at(then);
-    team.scratch = s.scratch;
-    const float2 teacher = stage_teacher<T, LANES>(a, row, s, team, row_at(row), entry);
-    entry = load_entry(a, then, lane);
-    Row r;
-    if constexpr (LOSS) {
-      constexpr int EACH = NV < 2 ? NV : 2;
-      Running run;
-#pragma unroll
-      for (int u = 0; u < NV; u += EACH) {
-        if (u > full) continue;
-        if constexpr (LANES > 64) {
-#pragma unroll
-          for (int i = u; i < u + EACH; ++i)
-            if (!mine_too(i)) raw[i] = none;
-        }
-        add_vectors<T, EACH>(a, s, raw + u, lane, u * LANES, LANES, whole, run);
-      }
-      if (rest_elements) add_vectors<T, 1>(a, s, &cut, whole, 0, 0, cuts ? items : 0, run);
-      find_logit(a, next_at, entry);
-      run = join<LANES>(a, team, run);
-      r = finish_loss<LANES>(a, row, s, team, teacher, run.max, run.rest, run.top);
-    } else {
-      find_logit(a, next_at, entry);
-      r = row_of_stats(a, row);
+    const T* then_at = row_at(then);
+    const float then_unit = scale * a.temperature;
+    if (next < a.rows) {
+      team.scratch = other.scratch;
+      teacher = stage_teacher<T, LANES>(a, next, other, team, then_at, entry);
+    } else if (!GRAD) {
+      return;
     }
+    const int64_t after = unmasked(then + rows_step), after_then = after < a.rows ? after : then;
+    entry = load_entry(a, after_then, lane);
+    Running run;
     if constexpr (GRAD) {
       T* grad = static_cast<T*>(a.grad) + row * a.grad_stride;
       float v[V];
       gradient<T>(a, r, unit, cut, v);
       if (cuts) store_vec<T, V>(grad + whole * V, v, rest_elements);
-      cut = load_the_cut(then, next_at);
+      cut = load_the_cut(then, then_at);
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
         if ((LANES > 64 && u < NV / 2) || u <= full) {
@@ -516,17 +529,31 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
             else store_vec<T, V>(to, v, V);
           }
         }
-        raw[u] = load(next_at, u);
+        raw[u] = load(then_at, u);
+        if constexpr (LOSS) {
+          if ((u + 1) % EACH == 0 && u + 1 - EACH >= LAG) add(other, u + 1 - EACH - LAG, run);
+        }
       }
       store_places<T, LANES>(a, s, team, r, unit, grad);
+      if (next >= a.rows) return;
     } else {
-      cut = load_the_cut(then, next_at);
+      cut = load_the_cut(then, then_at);
 #pragma unroll
-      for (int u = 0; u < NV; ++u) raw[u] = load(next_at, u);
+      for (int u = 0; u < NV; ++u) raw[u] = load(then_at, u);
     }
-    if (next >= a.rows) return;
-    row = next;
-    team.sync();  // (the next row's teacher takes this one's place)
+    if constexpr (LOSS) {
+#pragma unroll
+      for (int u = GRAD ? NV - LAG : 0; u < NV; u += EACH) add(other, u, run);
+      find_logit(a, row_at(after_then), entry);
+      r = finish(next, other, teacher, run);
+    } else {
+      find_logit(a, row_at(after_then), entry);
+      r = row_of_stats(a, next);
+      team.sync();  // (the row after the next takes this one's place in LDS)
+    }
+    const RowSpace was = s;
+    s = other, other = was;
+    row = next, next = after, unit = then_unit;
   }
 }
 
@@ -585,26 +612,36 @@ __global__ __launch_bounds__(LANES) void distill_stream(DistillArgs a) {
   }
 }
 
+// More than 64 KB of dynamic LDS has to be asked for.
+template <typename K>
+hipError_t allow_lds(K kernel, int bytes) {
+  if (bytes <= 65536) return hipSuccess;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 template <typename T, int NV, int LANES>
 hipError_t run_rows(const DistillArgs& a, int items, int per_unit, hipStream_t s) {
   constexpr int TEAMS = LANES == 64 ? 4 : 1;
-  const int space = row_space_bytes(a.top, items, a.tail);
+  const int space = row_space_bytes(a.top, items, a.tail), bytes = TEAMS * 2 * space;  // (two rows' at once)
   const int64_t blocks = (a.rows + TEAMS - 1) / TEAMS, most = 256 * (int64_t)per_unit;
   const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(LANES == 64 ? 256 : LANES);
-  if (a.loss && a.grad) distill_rows<T, NV, LANES, true, true><<<grid, block, TEAMS * space, s>>>(a, space);
-  else if (a.grad) distill_rows<T, NV, LANES, false, true><<<grid, block, TEAMS * space, s>>>(a, space);
-  else if constexpr (LANES == 64) distill_rows<T, NV, LANES, true, false><<<grid, block, TEAMS * space, s>>>(a, space);
-  return hipGetLastError();
+  auto run = [&](auto kernel) {
+    const hipError_t e = allow_lds(kernel, bytes);
+    if (e != hipSuccess) return e;
+    kernel<<<grid, block, bytes, s>>>(a, space);
+    return hipGetLastError();
+  };
+  if (a.loss && a.grad) return run(distill_rows<T, NV, LANES, true, true>);
+  if (a.grad) return run(distill_rows<T, NV, LANES, false, true>);
+  if constexpr (LANES == 64) return run(distill_rows<T, NV, LANES, true, false>);
+  return hipErrorInvalidValue;
 }
 
 template <typename T, int LANES>
 hipError_t run_stream(const DistillArgs& a, int items, hipStream_t s) {
   const int space = row_space_bytes(a.top, items, a.tail);
-  if (space > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(distill_stream<T, LANES>),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, space);
-    if (e != hipSuccess) return e;
-  }
+  const hipError_t e = allow_lds(distill_stream<T, LANES>, space);
+  if (e != hipSuccess) return e;
   distill_stream<T, LANES><<<dim3((unsigned)a.rows), LANES, space, s>>>(a);
   return hipGetLastError();
 }
@@ -613,6 +650,9 @@ template <typename T>
 hipError_t run_distill(const DistillArgs& a, hipStream_t s) {
   const int items = (a.classes + kVec<T> - 1) / kVec<T>;
   // vectors of a lane, threads, and workgroups that a compute unit holds at once
+  // (a wave to a row, four waves to a workgroup: up to some 380 entries a row)
+  const bool waves = 8 * row_space_bytes(a.top, items, a.tail) <= 65536;
+  if (items <= 256 && !waves) return run_stream<T, 256>(a, items, s);
   if (items <= 64) return run_rows<T, 1, 64>(a, items, 8, s);
   if (items <= 128) return run_rows<T, 2, 64>(a, items, 8, s);
   if (items <= 256) return run_rows<T, 4, 64>(a, items, 6, s);

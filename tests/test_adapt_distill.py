@@ -118,6 +118,30 @@ def test_loss_and_gradient(shape, dtype, tail):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(6, 1500, 700), (2300, 300, 9), (2200, 4099, 17), (2200, 9001, 33), (1100, 17001, 260),
+                                   (1100, 40003, 33), (600, 70001, 64)])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("tail", [False, True])
+def test_several_rows_to_a_workgroup(shape, dtype, tail):
+    """Rows enough that a workgroup takes several, one ahead of the other, masked ones between them."""
+    from paper_2407_02913_amd import adapt
+
+    print("distill", shape, dtype, tail, flush=True)
+    logits, values, index, row_scale = make(shape, dtype, tail, 4, not tail, True)
+    row_scale[torch.rand(shape[0], generator=torch.Generator().manual_seed(5)).cuda() < 0.3] = 0.0
+    row_scale[0] = row_scale[-1] = 1.5
+    logits[row_scale == 0] = math.nan
+    how = {"row_scale": row_scale, "temperature": 1.3, "tail": tail}
+    want = definition(logits, values, index, 1.3, tail)
+    both = adapt.distill_loss_and_grad(logits, values, index, **how)
+    check(both, want, dtype, row_scale, 1.3)
+    loss, stats = adapt.distill_loss(logits, values, index.to(torch.int32), **how)
+    check((loss, adapt.distill_grad(logits, values, index.to(torch.int32), stats, **how)), want, dtype, row_scale, 1.3)
+    again = logits.clone()
+    assert torch.equal(adapt.distill_loss_and_grad(again, values, index, out=again, **how)[1], both[1])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("classes", [37, 1000, 20011, 140001])
 def test_gradient_against_differences(classes, tail):
