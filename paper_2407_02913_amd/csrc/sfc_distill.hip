@@ -409,12 +409,18 @@ __device__ __forceinline__ float uniform(float v) {
 }
 
 // A row to a team, NV vectors to a lane.  A team takes every gridDim.x-th row, and loads a vector of its next one as soon
-// as the gradient of that vector has left: reading runs beside the exponentials and the writing.  A wave's loads and
-// stores are counted in one line, and it can wait for the ones at its front only where their number is known when this
-// is compiled: a workgroup's loads have no branches (more than half of its NV vectors are the row's for every lane, or
-// a smaller NV had been taken), and what else a row needs is loaded ahead of its logits or by scalar loads.
-// Addresses are a scalar for the team and a lane's offset, so that the registers are the row's; the vector that the
-// row's end cuts, if any, is loaded and stored by itself.
+// as the gradient of that vector has left: reading runs beside the exponentials and the writing.  Of long rows (NV =
+// 32) the sums, too, are made there, LAG vectors behind the loads, so that a wave has exponentials to work on where the
+// memory keeps it waiting; of shorter ones several workgroups share a compute unit and do that for each other.
+//
+// A wave's loads and stores are counted in one line, and it can wait for the ones at its front only where their number
+// is known when this is compiled: a workgroup's loads have no branches (at least half of its NV vectors are the row's for
+// every lane, or a smaller NV had been taken), and what else a row needs is loaded ahead of its logits or by scalar
+// loads.  Addresses are a scalar for the team and a lane's offset, so that the registers are the row's; the vector that
+// the row's end cuts, if any, is loaded and stored by itself.
+//
+// Bound by memory: 4096 rows of 131072 classes in bfloat16, loss and gradient 463 us (4.6 TB/s), the gradient alone 425
+// (5.1), where a copy of 1 GiB to 1 GiB comes to 4.8 to 5.1.
 template <typename T, int NV, int LANES, bool LOSS, bool GRAD>
 __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256 ? 3 : 4) : NV == 8 ? 4 : 2) void distill_rows(DistillArgs a, int space) {
   constexpr int V = kVec<T>;
@@ -557,7 +563,9 @@ __global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256
   }
 }
 
-// A row to a workgroup, read once for its sums and once more for the gradient.
+// A row to a workgroup, read once for its sums and once more for the gradient, then mostly out of the caches.  64 rows of
+// 1000 float32 classes are a wave's (distill_rows), 7.4 us; 64 rows of 32000 in bfloat16 here 13.7 us, the latency of
+// two passes, 4096 rows of 65536 the loss alone 99 us (5.4 TB/s).
 template <typename T, int LANES>
 __global__ __launch_bounds__(LANES) void distill_stream(DistillArgs a) {
   constexpr int V = kVec<T>;
@@ -657,12 +665,13 @@ hipError_t run_distill(const DistillArgs& a, hipStream_t s) {
   if (items <= 128) return run_rows<T, 2, 64>(a, items, 8, s);
   if (items <= 256) return run_rows<T, 4, 64>(a, items, 6, s);
   // Rows that are read again: where there are too few for the others to work in a pipeline, the more waves the better
-  // (64 rows of 32000 classes in 16 bits, loss and gradient: 12.7 us, kept in registers 14.1; 300 of 131072: 52 and 66).
+  // (300 rows of 131072 classes in 16 bits, loss and gradient: 59 us, kept in registers 72; 512 of 65536: 46 and 48; but
+  // 600 of 65536: 55 and 54).
   if (a.rows <= 512 || items > 16384) return run_stream<T, 512>(a, items, s);
   // Small workgroups, a row each, hide each other's waiting where little would be saved by keeping the row.  The loss
   // alone reads it once either way (4096 rows of 65536: 98 us, kept in registers 124).  The gradient alone needs no sums
-  // (777 rows of 32003: 25 and 29, 4096 rows of 16384: 60 and 65; but 4096 rows of 32000: 123 and 107).  Both: short
-  // rows (4096 rows of 6000: 41 and 46; of 16384: 75 and 71, of 131072: 660 and 532).
+  // (777 rows of 32003: 35 and 37, 4096 rows of 16384: 62 and 61; but 4096 rows of 24000: 92 and 86).  Both: short
+  // rows (4096 rows of 6000: 38 and 44; but of 10000: 54 and 50, of 32000: 156 and 123, of 131072: 668 and 463).
   if (!a.grad || (!a.loss ? items <= 2048 || a.rows <= 1024 : items <= 1024)) return run_stream<T, 256>(a, items, s);
   if (items <= 2048) return run_rows<T, 8, 256>(a, items, 4, s);
   if (items <= 4096) return run_rows<T, 16, 256>(a, items, 3, s);
