@@ -176,7 +176,7 @@ __device__ __forceinline__ float block_sum(float v, float* scratch) {
 // the mean of means, then squares about it, so nothing large is subtracted.
 __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g, int lane, int width) {
   const float4* part = reinterpret_cast<const float4*>(a.part) + ((int64_t)n * a.G + g) * a.chunks;
-  constexpr int KEPT = 4;  // parts of a lane that need no second read
+  constexpr int KEPT = 8;  // parts of a lane that need no second read
   float4 kept[KEPT];
   float sum = 0.0f, squares = 0.0f;
 #pragma unroll
@@ -186,6 +186,7 @@ __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g,
   }
 #pragma unroll
   for (int k = 0; k < KEPT; ++k) sum = fmaf(kept[k].x, kept[k].z, sum);
+#pragma unroll 4
   for (int i = lane + KEPT * width; i < a.chunks; i += width) {
     const float4 p = part[i];
     sum = fmaf(p.x, p.z, sum);
@@ -197,6 +198,7 @@ __device__ __forceinline__ float2 combine_parts(const NormArgs& a, int n, int g,
     const float d = kept[k].x - mean;
     squares += lane + k * width < a.chunks ? fmaf(d * d, kept[k].z, kept[k].y) : 0.0f;
   }
+#pragma unroll 4
   for (int i = lane + KEPT * width; i < a.chunks; i += width) {
     const float4 p = part[i];
     const float d = p.x - mean;

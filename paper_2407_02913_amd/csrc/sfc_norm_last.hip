@@ -339,7 +339,7 @@ __device__ __forceinline__ void back_vector(const NormArgs& a, const raw4& x, co
 }
 
 // Sums of a part of the pixels: of each channel (part_c: dz, dz h) and of each group (part: w dz, w dz h).
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kMost<T>) void last_back_sums(NormArgs a) {
   constexpr int V = kVec<T>;
   extern __shared__ float4 lds[];
@@ -360,18 +360,18 @@ __global__ __launch_bounds__(kMost<T>) void last_back_sums(NormArgs a) {
     s1[j] = s2[j] = 0.0f;
   }
   if (k.valid) {
-    for (int p = first + k.row; p < last; p += 2 * k.rows) {
-      raw4 rx[2], ry[2];
+    for (int p = first + k.row; p < last; p += 4 * k.rows) {
+      raw4 rx[4], ry[4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 4; ++u) {
         const int q = p + u * k.rows;
         if (q < last) {
-          rx[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
-          ry[u] = load_cut(dy + q * a.ys_r, k.valid, room_y - q * a.ys_r);
+          rx[u] = load_column<T, WHOLE>(x + q * a.xs_r, k, room - q * a.xs_r);
+          ry[u] = load_column<T, WHOLE>(dy + q * a.ys_r, k, room_y - q * a.ys_r);
         }
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < 4; ++u) {
         if (p + u * k.rows < last) {
           float h[V], dz[V];
           back_vector<T>(a, rx[u], ry[u], mean, rstd, w, b, h, dz);
@@ -434,7 +434,7 @@ __device__ __forceinline__ void store_dx(const NormArgs& a, const float (&rstd)[
   store_out<T, V>(a, dx, v, valid);
 }
 
-template <typename T>
+template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   constexpr int V = kVec<T>;
   extern __shared__ float4 lds[];
@@ -451,6 +451,29 @@ __global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   T* dx = static_cast<T*>(a.y) + n * a.xs_n + k.c;
   const int64_t room = a.x_end - n * a.xs_n - k.c, room_y = a.y_end - n * a.ys_n - k.c;
   float2* means = reinterpret_cast<float2*>(lds);
+  raw4 rx[2], ry[2];
+  int p = first + k.row;
+  auto load = [&]() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int q = p + u * k.rows;
+      if (q < last) {
+        rx[u] = load_column<T, WHOLE>(x + q * a.xs_r, k, room - q * a.xs_r);
+        ry[u] = load_column<T, WHOLE>(dy + q * a.ys_r, k, room_y - q * a.ys_r);
+      }
+    }
+  };
+  // (the first pixels, the weights and the statistics are on their way while the parts are joined)
+  if (k.valid) load();
+  float w[V], b[V], mean[V], rstd[V], c1[V], c2[V];
+  int group[V];
+  affine_of<T>(a, k, w, b);
+  groups_of<T>(a, k, group);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 s = reinterpret_cast<const float2*>(a.stats)[(int64_t)n * a.G + k.g0 + group[j]];
+    mean[j] = s.x, rstd[j] = s.y;
+  }
   const float inv = inverse((float)a.cpg * (float)a.P);
   const int width = lanes_of(k.groups), lane = threadIdx.x & (width - 1);
   for (int g = threadIdx.x / width; g < k.groups; g += (int)blockDim.x / width) {
@@ -462,35 +485,20 @@ __global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   }
   __syncthreads();
   if (!k.valid) return;
-  float w[V], b[V], mean[V], rstd[V], c1[V], c2[V];
-  int group[V];
-  affine_of<T>(a, k, w, b);
-  groups_of<T>(a, k, group);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const float2 s = reinterpret_cast<const float2*>(a.stats)[(int64_t)n * a.G + k.g0 + group[j]];
-    mean[j] = s.x, rstd[j] = s.y;
-    c1[j] = means[group[j]].x, c2[j] = means[group[j]].y;
-  }
-  for (int p = first + k.row; p < last; p += 2 * k.rows) {
-    raw4 rx[2], ry[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int q = p + u * k.rows;
-      if (q < last) {
-        rx[u] = load_cut(x + q * a.xs_r, k.valid, room - q * a.xs_r);
-        ry[u] = load_cut(dy + q * a.ys_r, k.valid, room_y - q * a.ys_r);
-      }
-    }
+  for (int j = 0; j < V; ++j) c1[j] = means[group[j]].x, c2[j] = means[group[j]].y;
+  while (p < last) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int q = p + u * k.rows;
       if (q < last) {
         float h[V], dz[V];
         back_vector<T>(a, rx[u], ry[u], mean, rstd, w, b, h, dz);
-        store_dx<T>(a, rstd, w, c1, c2, h, dz, dx + q * a.xs_r, k.valid);
+        store_dx<T>(a, rstd, w, c1, c2, h, dz, dx + q * a.xs_r, WHOLE ? V : k.valid);
       }
     }
+    p += 2 * k.rows;
+    load();
   }
 }
 
@@ -518,11 +526,13 @@ void set_parts(NormArgs* a, int x_size) {
   const int rows = a->threads >> a->lanes;
   const int64_t cells = (int64_t)a->N * a->slabs;
   int64_t parts = ((large ? 1024 : 2048) + cells - 1) / cells;
-  const int64_t most = a->P / (4 * rows) > 1 ? a->P / (4 * rows) : 1;
+  const int64_t most = (a->P + 4 * rows - 1) / (4 * rows);
   parts = parts < most ? parts : most;
   const int64_t joined = 4096 / a->slab > 1 ? 4096 / a->slab : 1;
   parts = parts < joined ? parts : joined;
   a->per = (int)((a->P + parts - 1) / parts);
+  // (few workgroups of long parts: twice the threads)
+  if (a->threads == 256 && cells * parts <= 512 && a->per > 8 * rows) a->threads = 512;
   a->chunks = (a->P + a->per - 1) / a->per;
   a->per_thread = 0;
 }
@@ -608,11 +618,15 @@ hipError_t run_last_back(NormArgs a, hipStream_t s) {
   constexpr int V = kVec<T>;
   const unsigned cells = (unsigned)((int64_t)a.N * a.slabs * a.chunks);
   const dim3 block((unsigned)a.threads);
-  last_back_sums<T><<<cells, block, rows_bytes(a, V) + (unsigned)(a.slab * a.cpg) * 8u, s>>>(a);
+  const unsigned sums = rows_bytes(a, V) + (unsigned)(a.slab * a.cpg) * 8u;
+  const bool whole = whole_vectors<T>(a);
+  if (whole) last_back_sums<T, true><<<cells, block, sums, s>>>(a);
+  else last_back_sums<T, false><<<cells, block, sums, s>>>(a);
   a.finals = a.dweight || a.dbias ? (a.C + 7) / 8 : 0;
-  const unsigned bytes = (unsigned)a.slab * 8u;
+  const unsigned bytes = (unsigned)a.slab * 8u > 1024u ? (unsigned)a.slab * 8u : 1024u;
   const dim3 grid(cells + (unsigned)a.finals);
-  last_back_apply<T><<<grid, block, bytes > 1024u ? bytes : 1024u, s>>>(a);
+  if (whole) last_back_apply<T, true><<<grid, block, bytes, s>>>(a);
+  else last_back_apply<T, false><<<grid, block, bytes, s>>>(a);
   return hipGetLastError();
 }
 
