@@ -106,8 +106,8 @@ def _check_norm(x, weight, bias):
             _misfit("weight, bias", f"float32 [{channels}] on {x.device}, contiguous, not {tuple(p.shape)} {p.dtype} on {p.device}")
 
 
-def _norm_forward(x, groups, weight, bias, eps, activation, dtype, y_scale, channels_last):
-    """(y, the buffer that holds the statistics, [N, groups, 2], and the workspace behind them)"""
+def _norm_forward(x, groups, weight, bias, eps, activation, dtype, y_scale, channels_last, stats):
+    """(y, the buffer that holds the statistics, [N, groups, 2], if asked for, and the workspace behind them)"""
     _check_norm(x, weight, bias)
     shape, stride, device = tuple(x.shape), x.stride(), x.device
     if channels_last is None and dtype is x.dtype and (
@@ -122,11 +122,13 @@ def _norm_forward(x, groups, weight, bias, eps, activation, dtype, y_scale, chan
         y = torch.empty(shape, dtype=dtype, device=device,
                         memory_format=torch.contiguous_format if planes else torch.channels_last)
     norm = _norm(shape, stride, x.dtype, y.stride(), dtype, groups, eps, activation, y_scale)
-    first = (shape[0] * groups + 1) // 2 * 4  # floats, 16 bytes and more
-    buffer = torch.empty(first + norm.forward_bytes // 4, dtype=torch.float32, device=device)
-    at = buffer.data_ptr()
-    _call(device, "sfc_group_norm", norm.at, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(), at,
-          at + 4 * first if norm.forward_bytes else None, norm.forward_bytes)
+    first = (shape[0] * groups + 1) // 2 * 4 if stats else 0  # floats, 16 bytes and more
+    space, buffer, at = norm.forward_bytes, None, None
+    if stats or space:
+        buffer = torch.empty(first + space // 4, dtype=torch.float32, device=device)
+        at = buffer.data_ptr()
+    _call(device, "sfc_group_norm", norm.at, x.data_ptr(), _ptr(weight), _ptr(bias), y.data_ptr(),
+          at if stats else None, at + 4 * first if space else None, space)
     return y, buffer
 
 
@@ -139,14 +141,15 @@ def group_norm_forward(x, groups, weight=None, bias=None, eps=1e-5, activation="
     weight and bias float32 [C] or None.  y has x's type and layout, or `dtype` (a 16-bit type from
     float32) and `channels_last`.  stats, float32 [N, groups, 2], are mean and 1 / sqrt(var + eps).
     activation: "none", "relu", "silu" or "gelu" (the exact one, with erf)."""
-    y, buffer = _norm_forward(x, groups, weight, bias, eps, activation, dtype or x.dtype, 0.0, channels_last)
+    y, buffer = _norm_forward(x, groups, weight, bias, eps, activation, dtype or x.dtype, 0.0, channels_last,
+                              True)
     return y, buffer.as_strided((x.shape[0], groups, 2), (2 * groups, 2, 1))
 
 
 def group_norm_i8(x, groups, weight=None, bias=None, eps=1e-5, activation="relu", *, y_scale):
     """The next convolution's activations: y of group_norm_forward as int8 planes,
     clamp(round-half-even(y / y_scale), -127, 127)."""
-    return _norm_forward(x, groups, weight, bias, eps, activation, torch.int8, float(y_scale), False)[0]
+    return _norm_forward(x, groups, weight, bias, eps, activation, torch.int8, float(y_scale), False, False)[0]
 
 
 def group_norm_backward(dy, x, stats, groups, weight=None, bias=None, eps=1e-5, activation="none"):
@@ -194,7 +197,7 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, activation="none"):
     """y of group_norm_forward, in x's type and layout; differentiable in x, weight and bias."""
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, weight, bias)):
         return _GroupNorm.apply(x, weight, bias, groups, eps, activation)
-    return _norm_forward(x, groups, weight, bias, eps, activation, x.dtype, 0.0, None)[0]
+    return _norm_forward(x, groups, weight, bias, eps, activation, x.dtype, 0.0, None, False)[0]
 
 
 # ---- low-rank adapters ----
@@ -215,6 +218,8 @@ _lowrank = lru_cache(maxsize=1024)(_Lowrank)
 
 
 def _row_stride(t, what):
+    if t.is_contiguous():
+        return 0
     rows, columns = t.shape
     stride = t.stride()
     if columns > 1 and stride[1] != 1:
@@ -317,6 +322,10 @@ def adapters(base, x, ids, down, up, scale=None):
 
 # ---- distillation from a teacher's top logits ----
 
+def _like(t):
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 @lru_cache(maxsize=1024)
 def _distill(rows, classes, top, dtype, wide, tail, temperature, logits_stride, grad_stride, values_stride, index_stride):
     return binding.DistillDesc(rows, classes, top, _TYPE[dtype], int(wide), int(tail), temperature,
@@ -366,7 +375,7 @@ def distill_grad(logits, values, index, stats, row_scale=None, temperature=1.0, 
     desc = _check_distill(logits, values, index, row_scale, temperature, tail, out)
     if not _dense(stats, (logits.shape[0], 4), torch.float32, logits.get_device()):
         _misfit("stats", f"float32 [{logits.shape[0]}, 4] on {logits.device}, as distill_loss gave them")
-    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if out is None else out
+    grad = _like(logits) if out is None else out
     _call(logits.device, "sfc_distill_grad", C.addressof(desc), logits.data_ptr(), values.data_ptr(), index.data_ptr(), _ptr(row_scale),
           stats.data_ptr(), grad.data_ptr())
     return grad
@@ -376,7 +385,7 @@ def distill_loss_and_grad(logits, values, index, row_scale=None, temperature=1.0
     """(loss, gradient) as of distill_loss and distill_grad, the logits read once: for a training step whose loss
     is sum(row_scale loss)."""
     desc = _check_distill(logits, values, index, row_scale, temperature, tail, out)
-    grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device) if out is None else out
+    grad = _like(logits) if out is None else out
     loss = torch.empty(logits.shape[0], dtype=torch.float32, device=logits.device)
     _call(logits.device, "sfc_distill_loss_grad", C.addressof(desc), logits.data_ptr(), values.data_ptr(), index.data_ptr(),
           _ptr(row_scale), loss.data_ptr(), grad.data_ptr())

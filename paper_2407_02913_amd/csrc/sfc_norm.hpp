@@ -24,7 +24,7 @@ struct NormArgs {
   void* y;              // forward: y; backward: dx
   const float* weight;  // [C] or null: ones
   const float* bias;    // [C] or null: zeros
-  float* stats;         // [N][G][2]: mean, 1 / sqrt(var + eps)
+  float* stats;         // [N][G][2]: mean, 1 / sqrt(var + eps); forward: or NULL
   float* part;          // workspace: what the first of two kernels leaves for the second, by [N][G][chunks]:
                         // forward float4 (mean, sum of squares about it, count), backward float2
   float* part_c;        // backward: sums of a channel, float2, indexed by c_image, c_chunk, c_group

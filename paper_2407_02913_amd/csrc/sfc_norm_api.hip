@@ -106,7 +106,7 @@ sfc_status sfc_group_norm(const sfc_group_norm_desc* desc, const void* x_dev, co
   const sfc_status st = describe(desc, &a, &nothing);
   if (st != SFC_OK) return st;
   if (nothing) return SFC_OK;
-  if (!x_dev || !y_dev || !stats_dev) return SFC_EINVAL;
+  if (!x_dev || !y_dev) return SFC_EINVAL;
   if (!aligned(x_dev, type_size(desc->x_type)) || !aligned(y_dev, type_size(desc->y_type)) ||
       !aligned(weight_dev, 4) || !aligned(bias_dev, 4) || !aligned(stats_dev, 8) || !aligned(workspace_dev, 16))
     return SFC_EINVAL;

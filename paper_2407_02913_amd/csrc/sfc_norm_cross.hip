@@ -56,7 +56,7 @@ __global__ __launch_bounds__(256) void cross_apply(NormArgs a, int parts, int ti
     if ((t & (width - 1)) == 0) {
       of_group[g] = s;
       // (the tile that holds a group's first channel keeps its statistics)
-      if (part == 0 && (g0 + g) * a.cpg >= c0) reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + g0 + g] = s;
+      if (a.stats && part == 0 && (g0 + g) * a.cpg >= c0) reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + g0 + g] = s;
     }
   }
   __syncthreads();

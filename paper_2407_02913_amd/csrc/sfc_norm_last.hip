@@ -174,7 +174,7 @@ __global__ __launch_bounds__(1024) void last_resident(NormArgs a) {
   float rstd[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) rstd[j] = inverse_sqrt(fmaf(rstds[group[j]], inv, a.eps));
-  for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
+  for (int g = threadIdx.x; a.stats && g < k.groups; g += (int)blockDim.x)
     reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] =
         make_float2(means[g] * inv, inverse_sqrt(fmaf(rstds[g], inv, a.eps)));
 #pragma unroll
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kMost<TI>) void last_apply(NormArgs a) {
   TO* y = static_cast<TO*>(a.y) + n * a.ys_n + k.c;
   const int64_t room = a.x_end - n * a.xs_n - k.c;
   slab_stats(a, n, k.g0, k.groups, stat);
-  if (chunk == 0)
+  if (a.stats && chunk == 0)
     for (int g = threadIdx.x; g < k.groups; g += (int)blockDim.x)
       reinterpret_cast<float2*>(a.stats)[(int64_t)n * a.G + k.g0 + g] = stat[g];
   const int mine = last - first - k.row;
@@ -479,6 +479,7 @@ __global__ __launch_bounds__(kMost<T>) void last_back_apply(NormArgs a) {
   for (int g = threadIdx.x / width; g < k.groups; g += (int)blockDim.x / width) {
     const float2* part = reinterpret_cast<const float2*>(a.part) + ((int64_t)n * a.G + k.g0 + g) * a.chunks;
     float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 4
     for (int i = lane; i < a.chunks; i += width) s.x += part[i].x, s.y += part[i].y;
     for (int m = width >> 1; m; m >>= 1) s.x += __shfl_xor(s.x, m, 64), s.y += __shfl_xor(s.y, m, 64);
     if (lane == 0) means[g] = make_float2(s.x * inv, s.y * inv);

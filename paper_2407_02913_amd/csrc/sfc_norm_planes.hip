@@ -102,7 +102,7 @@ __global__ __launch_bounds__(1024) void planes_resident(NormArgs a) {
   }
   const float var = block_sum(squares, scratch + 16) * inv;
   const float2 stat = make_float2(mean, inverse_sqrt(var + a.eps));
-  if (t == 0) reinterpret_cast<float2*>(a.stats)[blockIdx.x] = stat;
+  if (a.stats && t == 0) reinterpret_cast<float2*>(a.stats)[blockIdx.x] = stat;
   TO* y = static_cast<TO*>(a.y) + y0;
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void planes_apply(NormArgs a) {
   TO* y = static_cast<TO*>(a.y) + y0;
   stage_affine(a, g, lds);
   const float2 stat = combine_parts(a, n, g, threadIdx.x & 63, 64);
-  if (chunk == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.stats)[ng] = stat;
+  if (a.stats && chunk == 0 && threadIdx.x == 0) reinterpret_cast<float2*>(a.stats)[ng] = stat;
   __syncthreads();
   for (int q = first + threadIdx.x; q < last; q += 1024) {
     raw4 r[4];
@@ -432,6 +432,7 @@ __global__ __launch_bounds__(256) void planes_back_apply(NormArgs a) {
   stage_affine(a, g, lds);
   const float2 stat = reinterpret_cast<const float2*>(a.stats)[ng];
   float2 s = make_float2(0.0f, 0.0f);
+#pragma unroll 4
   for (int i = threadIdx.x & 63; i < a.chunks; i += 64) {
     const float2 v = reinterpret_cast<const float2*>(a.part)[ng * a.chunks + i];
     s.x += v.x, s.y += v.y;

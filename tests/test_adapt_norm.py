@@ -252,6 +252,17 @@ def test_in_place_through_the_c_entry(layout, shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("shape", [(3, 46, 7, 9, 2), (1, 24, 131, 127, 1), (2, 64, 56, 56, 32)])
+def test_without_statistics(layout, shape):
+    from paper_2407_02913_amd import adapt
+
+    x, weight, bias, _ = make(shape, torch.float16, layout, seed=8)
+    want, _ = adapt.group_norm_forward(x, shape[4], weight, bias, activation="gelu")
+    assert torch.equal(adapt.group_norm(x, shape[4], weight, bias, activation="gelu"), want)
+
+
+@pytest.mark.gpu
 def test_one_value_to_a_group_has_no_gradient():
     from paper_2407_02913_amd import adapt
 
@@ -373,7 +384,7 @@ def test_bad_pointers_and_workspaces():
     big = 1 << 30
     assert lib.sfc_group_norm(at, None, None, None, 256, 256, 256, big, None) == 1
     assert lib.sfc_group_norm(at, 256, None, None, None, 256, 256, big, None) == 1
-    assert lib.sfc_group_norm(at, 256, None, None, 256, None, 256, big, None) == 1
+    assert lib.sfc_group_norm(at, 256, None, None, 256, None, None, big, None) == 6  # (without statistics, not a workspace)
     assert lib.sfc_group_norm(at, 258, None, None, 256, 256, 256, big, None) == 1
     assert lib.sfc_group_norm(at, 256, 2, None, 256, 256, 256, big, None) == 1
     assert lib.sfc_group_norm(at, 256, None, None, 256, 256, None, big, None) == 6
