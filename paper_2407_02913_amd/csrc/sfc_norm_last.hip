@@ -346,8 +346,8 @@ __device__ __forceinline__ void back_vector(const NormArgs& a, const raw4& x, co
 }
 
 // Sums of a part of the pixels: of each channel (part_c: dz, dz h) and of each group (part: w dz, w dz h).  32 bfloat16
-// images of 128 channels on 56x56, SiLU: 25 us (2.0 TB/s), and last_back_apply 28 (2.8): the activation's derivative, made
-// in both from x alone, takes some 11 of each.
+// images of 128 channels on 56x56, SiLU, both kernels 41 us (3.1 TB/s): the activation's derivative, made in both from x
+// alone, takes some 11 of each.
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kMost<T>) void last_back_sums(NormArgs a) {
   constexpr int V = kVec<T>;
@@ -526,8 +526,11 @@ void set_slab(NormArgs* a, int groups, int V) {
 }
 
 // Two kernels: as many whole groups as 256 threads have vector columns for (a wider group: more), and parts of the pixels
-// for some 1024 workgroups, each of at least 4 rows of threads.  Every workgroup of the second kernel joins the parts of
-// its image: where the maps are large, workgroups of 512 threads halve their number, and they stay below 4096 (64 KB).
+// for some 512 workgroups, each of at least 4 rows of threads; 1024 where the maps are large.  Every workgroup of the second
+// kernel joins the parts of its image, so that more of them read more: 32 bfloat16 images of 128 channels on 56x56, 32
+// groups, SiLU, forward 27.2 us and backward 41.0, with 2048 workgroups 34.6 and 53.3; eight on 112x112 27.0 and 41.3, else
+// 32.2 and 45.0 (but 50 float16 images of 23 channels on 41x77, one group, 24.5 and 32.6, else 23.6 and 30.1).  An image's
+// parts stay below 4096 (64 KB).
 void set_parts(NormArgs* a, int x_size) {
   const int V = 16 / x_size;
   const bool large = (int64_t)a->N * a->P * a->C >= ((int64_t)1 << 24);
@@ -535,7 +538,7 @@ void set_parts(NormArgs* a, int x_size) {
   set_slab(a, a->cpg < 256 * V ? 256 * V / a->cpg : 1, V);
   const int rows = a->threads >> a->lanes;
   const int64_t cells = (int64_t)a->N * a->slabs;
-  int64_t parts = ((large ? 1024 : 2048) + cells - 1) / cells;
+  int64_t parts = ((large ? 1024 : 512) + cells - 1) / cells;
   const int64_t most = (a->P + 4 * rows - 1) / (4 * rows);
   parts = parts < most ? parts : most;
   const int64_t joined = 4096 / a->slab > 1 ? 4096 / a->slab : 1;
