@@ -8,9 +8,10 @@
 // The logits are the largest tensor of a training step, and a row's gradient needs the whole row's sum: a row is
 // kept in registers as it was loaded (distill_rows: by a wave up to 256 vectors of 16 bytes, by a workgroup above),
 // so that loss and gradient read it once and write it once.  Rows past the registers are read twice, the second time
-// mostly out of the caches (distill_stream), and so are those of calls that gain nothing by keeping them (run_distill).  The gradient is stored as if there were no teacher, then the wave that
-// stored a place's vector stores that place once more.  With a tail the sum outside the top is added up as such (a
-// difference of sums would lose it where the top holds nearly all): a byte of LDS a vector tells its elements.
+// mostly out of the caches (distill_stream), and so are those of calls that gain nothing by keeping them (run_distill).
+// The gradient is stored as if there were no teacher, then the wave that stored a place's vector stores that place once
+// more.  With a tail the sum outside the top is added up as such (a difference of sums would lose it where the top holds
+// nearly all): a byte of LDS a vector tells its elements.
 #include "sfc_distill.hpp"
 
 namespace sfc {
@@ -182,8 +183,8 @@ __device__ __forceinline__ float2 stage_teacher(const DistillArgs& a, int64_t ro
   team.sync();
   if (a.grad) {
     // entries for one place, added in their order by each of them
-  #pragma unroll 1
-  for (int k = lane; k < a.top; k += size) {
+#pragma unroll 1
+    for (int k = lane; k < a.top; k += size) {
       const int mine = s.at[k];
       float all = 0.0f;
 #pragma unroll 4
@@ -422,7 +423,8 @@ __device__ __forceinline__ float uniform(float v) {
 // Bound by memory: 4096 rows of 131072 classes in bfloat16, loss and gradient 463 us (4.6 TB/s), the gradient alone 425
 // (5.1), where a copy of 1 GiB to 1 GiB comes to 4.8 to 5.1.
 template <typename T, int NV, int LANES, bool LOSS, bool GRAD>
-__global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? (LANES == 256 ? 3 : 4) : NV == 8 ? 4 : 2) void distill_rows(DistillArgs a, int space) {
+__global__ __launch_bounds__(LANES == 64 ? 256 : LANES, NV == 16 ? 3 : NV == 8 ? 4 : 2)
+void distill_rows(DistillArgs a, int space) {
   constexpr int V = kVec<T>;
   constexpr int TEAMS = LANES == 64 ? 4 : 1;
   extern __shared__ float4 lds[];
@@ -640,7 +642,8 @@ hipError_t run_rows(const DistillArgs& a, int items, int per_unit, hipStream_t s
     return hipGetLastError();
   };
   if (a.loss && a.grad) return run(distill_rows<T, NV, LANES, true, true>);
-  if (a.grad) return run(distill_rows<T, NV, LANES, false, true>);
+  if constexpr (NV != 8)  // (run_distill: the gradient alone of such rows is distill_stream's)
+    if (a.grad) return run(distill_rows<T, NV, LANES, false, true>);
   if constexpr (LANES == 64) return run(distill_rows<T, NV, LANES, true, false>);
   return hipErrorInvalidValue;
 }
